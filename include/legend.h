@@ -368,6 +368,153 @@ int legend_rank_edges_static(legend_ctx* ctx, const int64_t* src, const int32_t*
 /* Largest m legend_rank_edges_static accepts at embedding dimension dim (0: unsupported dim). */
 int64_t legend_rank_edges_static_max_triples(int32_t dim);
 
+/*
+ * Operators for the dense parts of a model: layer norm, and an AdamW step over many tensors.
+ *
+ * What is trained beside the tables (a head that reads learned rows, a projection, the weight and bias of a norm) lives
+ * in device memory of the caller.  These calls
+ *   - take DEVICE pointers owned by the caller, on the context's GPU, aligned to their element type;
+ *   - enqueue on the context's compute stream and return without waiting.  The caller orders its own streams with that one
+ *     (or hands its stream over as legend_config.compute_stream);
+ *   - allocate nothing, except for legend_adamw_create, and may be recorded into a HIP graph, except where said;
+ *   - leave the calling thread's current device as it was;
+ *   - give the same bits for the same inputs, whatever runs beside them.
+ * A context's rules hold (one thread at a time; LEGEND_E_HIP is final).  Per-kernel profiling does not cover them.
+ */
+/* Element types of the caller's device tensors: fp32, bfloat16, fp16.  Arithmetic is fp32, rounded to nearest at the end. */
+enum { LEGEND_TYPE_FLOAT = 0, LEGEND_TYPE_BFLOAT = 1, LEGEND_TYPE_HALF = 2 };
+
+/*
+ * Layer norm of `rows` rows of `dim` numbers:
+ *   mean = sum x / dim,  var = sum (x - mean)^2 / dim,  rstd = 1 / sqrt(var + eps),  xh = (x - mean) rstd,  y = xh weight + bias
+ * and, with u = dy weight,
+ *   dx = rstd (u - mean(u) - xh mean(u xh)),  dweight = sum over rows of dy xh,  dbias = sum over rows of dy.
+ * The rows are those of the matrix x, or (table >= 0) rows of a resident table: a head reads learned embeddings without
+ * passing through the host.  In a table's case a row whose id is out of range, or whose partition is not resident, sets
+ * bit 0 (bit 1) of *status, is written as zeros (y, mean, rstd, dx) and adds nothing to dweight and dbias; the call clears no
+ * bits, so that one look at *status covers many calls.  A table's call recorded into a graph reads the partitions where
+ * they were when it was recorded: record it again after a swap.
+ *
+ * One struct serves both directions: legend_layer_norm_forward reads the first three groups and writes the last line of the
+ * third and the fourth; legend_layer_norm_backward reads mean and rstd as the forward pass wrote them, and the fifth.
+ * Memory: outputs must not overlap anything else the call uses, except that y may be x itself, and dx may be x or dy itself
+ * (same address, stride and element size).
+ */
+typedef struct legend_layer_norm {
+    uint32_t struct_size;      /* sizeof(legend_layer_norm) of the caller                          */
+    int32_t  dim;              /* numbers per row, 1 .. 2^20                                       */
+    int64_t  rows;             /* >= 0                                                             */
+    const void* x;             /* [rows] rows, x_stride elements apart; NULL with a table          */
+    int64_t  x_stride;         /* >= dim, or 0: every row is the same one                          */
+    int32_t  x_type;           /* LEGEND_TYPE_*; with a table LEGEND_TYPE_FLOAT                    */
+    int32_t  table;            /* -1: rows of x; LEGEND_TABLE_NODE_EMB or LEGEND_TABLE_REL_EMB: rows
+                                  of the table, dim as in the context                              */
+    const int64_t* ids;        /* table: [rows] global node ids / relation ids, or NULL for 0, 1, .. */
+    uint32_t* status;          /* table: one word (required)                                       */
+    const void* weight;        /* [dim], or NULL for ones                                          */
+    const void* bias;          /* [dim], or NULL for zeros                                         */
+    int32_t  weight_type;      /* LEGEND_TYPE_* of weight and bias                                 */
+    float    eps;              /* > 0                                                              */
+    float*   mean;             /* [rows]; forward: may be NULL                                     */
+    float*   rstd;             /* [rows]; forward: may be NULL                                     */
+    void*    y;                /* forward: [rows] rows                                             */
+    int64_t  y_stride;         /* >= dim                                                           */
+    int32_t  y_type;           /* LEGEND_TYPE_FLOAT or x_type; any where x_type is LEGEND_TYPE_FLOAT */
+    int32_t  dy_type;          /* as y_type                                                        */
+    const void* dy;            /* backward: gradient of y                                          */
+    int64_t  dy_stride;        /* >= dim, or 0: every row is the same one                          */
+    void*    dx;               /* backward: gradient of the rows, x_type; NULL: not wanted         */
+    int64_t  dx_stride;        /* >= dim                                                           */
+    void*    dweight;          /* backward: [dim]; NULL: not wanted                                */
+    void*    dbias;            /* backward: [dim]; NULL: not wanted                                */
+    int32_t  dweight_type;     /* LEGEND_TYPE_* of dweight and dbias                               */
+    int32_t  accumulate;       /* 1: add to dweight and dbias instead of writing them              */
+    void*    workspace;        /* backward with dweight or dbias: at least legend_layer_norm_workspace
+                                  bytes, aligned to 16; calls that may overlap in time (graphs replayed
+                                  on two streams) need one each                                    */
+    int64_t  workspace_bytes;
+} legend_layer_norm;
+
+/* Errors of both: LEGEND_E_INVAL, LEGEND_E_STATE (a recorded call on a table while a swap is in flight or not yet seen: make
+ * one ordinary call first), LEGEND_E_HIP.  rows == 0 is fine (dweight and dbias become zero). */
+int legend_layer_norm_forward(legend_ctx* ctx, const legend_layer_norm* norm);
+int legend_layer_norm_backward(legend_ctx* ctx, const legend_layer_norm* norm);
+/* Bytes of workspace of a backward pass (-1: rows or dim out of range). */
+int64_t legend_layer_norm_workspace(int64_t rows, int32_t dim);
+
+/*
+ * AdamW over many tensors at once.  With t = steps made + 1, lr' = lr * *lr_factor * lr_scale, every element does
+ *   g = grad * *grad_scale * clip
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr' weight_decay) - lr' / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * (decoupled weight decay), where p is the master copy if there is one (the parameter then receives p rounded) and
+ *   norm = *grad_scale * sqrt(sum of grad^2 over all tensors)  (64 bits),
+ *   clip = max_norm > 0 and norm > max_norm ? max_norm / (norm + 1e-6) : 1.
+ * With max_norm > 0 or a norm output asked for, a step whose norm is not finite changes nothing and counts as skipped.
+ * Without both the norm is not computed and such gradients go through the formulas.
+ * The number of steps lives on the device, so that a recorded step replays as the next one.
+ *
+ * States: LEGEND_STATE_FLOAT: m, v [count] fp32.  LEGEND_STATE_BLOCK: 8 bits; m and v hold m and sqrt(v) as e4m3 codes (1 sign, 4
+ * exponent, 3 mantissa bits, largest 448; 0x7f and 0xff: NaN) in units of an fp32 scale for each block of 256 consecutive
+ * elements, scale = max |.| / 448 over the block's finite values (below 2^-100: 0, and the block's codes too).  The update of p uses the
+ * unrounded m and v.  A value x in units of the scale is rounded stochastically: up from the code below it with the
+ * probability of its fraction, so that moments which change by less than a code's step (beta2 = 0.999 changes sqrt(v) by
+ * 0.05 % a step, codes are 6 to 12 % apart) still follow on average.  The random word w of element e of tensor k at step t is a
+ * counter hash, w = mix(low32(e) ^ low32(e / 2^32) * 0x9E3779B1 ^ low32(fold(fold(seed, t), k))) with fold as in
+ * legend_init_partitions and mix(w): w ^= w >> 16, w *= 0x9E3779B1, w ^= w >> 15, w *= 0x85157AF5, w ^= w >> 16 (32 bits); m takes
+ * the fraction (w >> 12) / 2^20, sqrt(v) the fraction (w & 0xffff) / 2^16.  A sqrt(v) above zero is at least the smallest code
+ * above zero.  States of zeros (scales too) are the start.
+ */
+enum { LEGEND_STATE_FLOAT = 0, LEGEND_STATE_BLOCK = 1 };
+
+typedef struct legend_adamw legend_adamw;
+
+typedef struct legend_adamw_config {
+    uint32_t struct_size;      /* sizeof(legend_adamw_config) of the caller                        */
+    uint32_t reserved;         /* 0                                                                */
+    double   beta1, beta2;     /* in [0, 1)                                                        */
+    double   eps;              /* > 0                                                              */
+    double   max_norm;         /* 0: no clipping                                                   */
+    uint64_t seed;             /* of the stochastic rounding                                       */
+} legend_adamw_config;
+
+typedef struct legend_adamw_tensor {
+    void*       param;         /* [count] param_type                                               */
+    const void* grad;          /* [count] grad_type                                                */
+    float*      master;        /* [count] fp32, or NULL; only beside a 16-bit parameter            */
+    void*       m;             /* [count] fp32 or codes                                            */
+    void*       v;             /* [count] fp32 or codes                                            */
+    float*      m_scale;       /* LEGEND_STATE_BLOCK: [ceil(count / 256)], else NULL               */
+    float*      v_scale;       /* the same                                                         */
+    int64_t     count;         /* >= 0                                                             */
+    int32_t     param_type, grad_type;   /* LEGEND_TYPE_*                                          */
+    int32_t     state_type;    /* LEGEND_STATE_*                                                   */
+    uint32_t    reserved;      /* 0                                                                */
+    double      weight_decay;  /* >= 0                                                             */
+    double      lr_scale;      /* >= 0                                                             */
+} legend_adamw_tensor;
+
+/*
+ * An optimiser over n tensors: checks and copies the descriptions, allocates its tables (not the states) on the context's
+ * GPU.  Tensors, states and scales must stay valid; none of them may overlap another, gradients may overlap each other
+ * only.  Steps made: 0.  Errors: LEGEND_E_INVAL, LEGEND_E_NOMEM, LEGEND_E_STATE (the stream is recording), LEGEND_E_HIP.
+ */
+int legend_adamw_create(legend_ctx* ctx, const legend_adamw_config* cfg, const legend_adamw_tensor* tensors, int64_t n,
+                        legend_adamw** out);
+/* Waits for the optimiser's work and frees it.  It may come after legend_destroy of its context (every other call is then
+ * refused with LEGEND_E_STATE).  NULL is accepted. */
+int legend_adamw_destroy(legend_adamw* opt);
+/* One step.  lr >= 0; lr_factor and grad_scale: one fp32 each on the device, read when the step runs, or NULL for 1;
+ * norm: one fp32 on the device, or NULL. */
+int legend_adamw_step(legend_adamw* opt, double lr, const float* lr_factor, const float* grad_scale, float* norm);
+/* Other gradient buffers for the same tensors, in their order (types as at creation).  Waits for the compute stream; not
+ * while it is recording. */
+int legend_adamw_set_gradients(legend_adamw* opt, const void* const* grads, int64_t n);
+/* Steps made and steps skipped; both wait for the compute stream and are refused while it is recording.  Setting clears the
+ * count of skipped steps. */
+int legend_adamw_get_steps(legend_adamw* opt, int64_t* steps, int64_t* skipped);
+int legend_adamw_set_steps(legend_adamw* opt, int64_t steps);
+
 /* Message of the last error on this thread ("" if none). */
 const char* legend_last_error(void);
 

@@ -25,6 +25,8 @@ CORRUPT_DST, CORRUPT_SRC, CORRUPT_BOTH = 0, 1, 2
 UPDATE_DETERMINISTIC, UPDATE_ATOMIC = 0, 1
 MEM_HOST, MEM_DEVICE = 0, 1
 TABLE_NODE_EMB, TABLE_NODE_STATE, TABLE_REL_EMB, TABLE_REL_STATE = 0, 1, 2, 3
+TYPE_FLOAT, TYPE_BFLOAT, TYPE_HALF = 0, 1, 2
+STATE_FLOAT, STATE_BLOCK = 0, 1
 
 EXPORTS = [
     "legend_init_partitions", "legend_destroy", "legend_swap_partition", "legend_partition_slot",
@@ -32,6 +34,9 @@ EXPORTS = [
     "legend_rank_edges_static_max_triples", "legend_read_embeddings", "legend_debug_batch_indices",
     "legend_plan_order", "legend_sync", "legend_profile_enable", "legend_profile_read",
     "legend_profile_name", "legend_batch_shape_of", "legend_unique_rows_read", "legend_fallback_chunks_read",
+    "legend_layer_norm_forward", "legend_layer_norm_backward", "legend_layer_norm_workspace",
+    "legend_adamw_create", "legend_adamw_destroy", "legend_adamw_step", "legend_adamw_set_gradients",
+    "legend_adamw_get_steps", "legend_adamw_set_steps",
     "legend_last_error",
 ]
 
@@ -71,6 +76,32 @@ class legend_batch_shape(C.Structure):
                 ("key_bits", C.c_int32), ("row_tiles", C.c_int32)]
 
 
+class legend_layer_norm(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dim", C.c_int32), ("rows", C.c_int64),
+        ("x", C.c_void_p), ("x_stride", C.c_int64), ("x_type", C.c_int32), ("table", C.c_int32),
+        ("ids", C.c_void_p), ("status", C.c_void_p),
+        ("weight", C.c_void_p), ("bias", C.c_void_p), ("weight_type", C.c_int32), ("eps", C.c_float),
+        ("mean", C.c_void_p), ("rstd", C.c_void_p),
+        ("y", C.c_void_p), ("y_stride", C.c_int64), ("y_type", C.c_int32), ("dy_type", C.c_int32),
+        ("dy", C.c_void_p), ("dy_stride", C.c_int64), ("dx", C.c_void_p), ("dx_stride", C.c_int64),
+        ("dweight", C.c_void_p), ("dbias", C.c_void_p), ("dweight_type", C.c_int32), ("accumulate", C.c_int32),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
+    ]
+
+
+class legend_adamw_config(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("reserved", C.c_uint32), ("beta1", C.c_double), ("beta2", C.c_double),
+                ("eps", C.c_double), ("max_norm", C.c_double), ("seed", C.c_uint64)]
+
+
+class legend_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("master", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("count", C.c_int64), ("param_type", C.c_int32),
+                ("grad_type", C.c_int32), ("state_type", C.c_int32), ("reserved", C.c_uint32),
+                ("weight_decay", C.c_double), ("lr_scale", C.c_double)]
+
+
 class LegendError(RuntimeError):
     def __init__(self, code: int, message: str):
         super().__init__(f"legend error {code}: {message}")
@@ -107,11 +138,21 @@ def _load() -> C.CDLL:
     lib.legend_batch_shape_of.argtypes = [vp, C.POINTER(legend_batch_shape)]
     lib.legend_unique_rows_read.argtypes = [vp, C.POINTER(i64), C.POINTER(i64)]
     lib.legend_fallback_chunks_read.argtypes = [vp, C.POINTER(i64)]
+    lib.legend_layer_norm_forward.argtypes = [vp, C.POINTER(legend_layer_norm)]
+    lib.legend_layer_norm_backward.argtypes = [vp, C.POINTER(legend_layer_norm)]
+    lib.legend_layer_norm_workspace.argtypes = [i64, i32]
+    lib.legend_adamw_create.argtypes = [vp, C.POINTER(legend_adamw_config), vp, i64, C.POINTER(vp)]
+    lib.legend_adamw_destroy.argtypes = [vp]
+    lib.legend_adamw_step.argtypes = [vp, C.c_double, vp, vp, vp]
+    lib.legend_adamw_set_gradients.argtypes = [vp, vp, i64]
+    lib.legend_adamw_get_steps.argtypes = [vp, C.POINTER(i64), C.POINTER(i64)]
+    lib.legend_adamw_set_steps.argtypes = [vp, i64]
     lib.legend_last_error.restype = C.c_char_p
     for name in EXPORTS:
         if name not in ("legend_profile_name", "legend_last_error", "legend_rank_edges_static_max_triples"):
             getattr(lib, name).restype = C.c_int
     lib.legend_rank_edges_static_max_triples.restype = C.c_int64
+    lib.legend_layer_norm_workspace.restype = C.c_int64
     return lib
 
 
@@ -355,3 +396,65 @@ def legend_unique_rows_read(ctx):
     u, b = C.c_int64(0), C.c_int64(0)
     _check(_lib.legend_unique_rows_read(ctx, C.byref(u), C.byref(b)))
     return u.value, b.value
+
+
+def make_layer_norm(*, rows, dim, x=None, x_stride=None, x_type=TYPE_FLOAT, table=-1, ids=None, status=None, weight=None,
+                    bias=None, weight_type=TYPE_FLOAT, eps=1e-5, mean=None, rstd=None, y=None, y_stride=None, y_type=None,
+                    dy=None, dy_stride=None, dy_type=None, dx=None, dx_stride=None, dweight=None, dbias=None,
+                    dweight_type=TYPE_FLOAT, accumulate=False, workspace=None, workspace_bytes=0) -> legend_layer_norm:
+    """Arguments of both directions, kept and used again by a program whose buffers stay.  Pointers are device addresses
+    (integers; None passes NULL); strides default to dim, y_type and dy_type to x_type."""
+    return legend_layer_norm(
+        C.sizeof(legend_layer_norm), dim, rows, x, dim if x_stride is None else x_stride, x_type, table, ids, status, weight, bias,
+        weight_type, eps, mean, rstd, y, dim if y_stride is None else y_stride, x_type if y_type is None else y_type,
+        x_type if dy_type is None else dy_type, dy, dim if dy_stride is None else dy_stride, dx, dim if dx_stride is None else dx_stride,
+        dweight, dbias, dweight_type, int(accumulate), workspace, workspace_bytes)
+
+
+def legend_layer_norm_forward(ctx, norm: legend_layer_norm) -> None:
+    _check(_lib.legend_layer_norm_forward(ctx, norm))
+
+
+def legend_layer_norm_backward(ctx, norm: legend_layer_norm) -> None:
+    _check(_lib.legend_layer_norm_backward(ctx, norm))
+
+
+def legend_layer_norm_workspace(rows: int, dim: int) -> int:
+    return int(_lib.legend_layer_norm_workspace(rows, dim))
+
+
+def make_adamw_tensor(*, count, param, grad, m, v, m_scale=None, v_scale=None, master=None, param_type=TYPE_FLOAT,
+                      grad_type=TYPE_FLOAT, state_type=STATE_FLOAT, weight_decay=0.0, lr_scale=1.0) -> legend_adamw_tensor:
+    """Pointers are device addresses (integers; None passes NULL)."""
+    return legend_adamw_tensor(param, grad, master, m, v, m_scale, v_scale, count, param_type, grad_type, state_type, 0, weight_decay, lr_scale)
+
+
+def legend_adamw_create(ctx, tensors: Sequence[legend_adamw_tensor], *, beta1=0.9, beta2=0.999, eps=1e-8, max_norm=0.0, seed=0):
+    cfg = legend_adamw_config(C.sizeof(legend_adamw_config), 0, beta1, beta2, eps, max_norm, seed & ((1 << 64) - 1))
+    handle = C.c_void_p()
+    _check(_lib.legend_adamw_create(ctx, C.byref(cfg), (legend_adamw_tensor * max(len(tensors), 1))(*tensors), len(tensors), C.byref(handle)))
+    return handle
+
+
+def legend_adamw_destroy(opt) -> None:
+    _check(_lib.legend_adamw_destroy(opt))
+
+
+def legend_adamw_step(opt, lr: float, lr_factor: Optional[int] = None, grad_scale: Optional[int] = None, norm: Optional[int] = None) -> None:
+    """lr_factor, grad_scale and norm are device addresses of one float each, or None."""
+    _check(_lib.legend_adamw_step(opt, lr, lr_factor, grad_scale, norm))
+
+
+def legend_adamw_set_gradients(opt, grads: Sequence[Optional[int]]) -> None:
+    _check(_lib.legend_adamw_set_gradients(opt, (C.c_void_p * max(len(grads), 1))(*grads), len(grads)))
+
+
+def legend_adamw_get_steps(opt):
+    """(steps made, steps skipped)"""
+    steps, skipped = C.c_int64(0), C.c_int64(0)
+    _check(_lib.legend_adamw_get_steps(opt, C.byref(steps), C.byref(skipped)))
+    return steps.value, skipped.value
+
+
+def legend_adamw_set_steps(opt, steps: int) -> None:
+    _check(_lib.legend_adamw_set_steps(opt, steps))

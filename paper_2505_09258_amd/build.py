@@ -19,7 +19,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "liblegend_hip.so")
 
 SOURCES = ["runtime.hip", "kernels_prepare.hip", "kernels_sort.hip", "kernels_chunk.hip", "kernels_chunk_gemm.hip", "kernels_chunk_split.hip",
-           "kernels_update.hip", "kernels_rank.hip", "kernels_chunk_trans.hip", "order_plan.cpp"]
+           "kernels_update.hip", "kernels_rank.hip", "kernels_chunk_trans.hip", "order_plan.cpp", "dense.hip",
+           "kernels_norm.hip", "kernels_adamw.hip"]
 # translation units of one source with one value of a macro each: source, macro, values
 VARIANTS = [("kernels_chunk_split.hip", "LEGEND_SPLIT_NJ", (2, 4, 6, 7, 8))]
 

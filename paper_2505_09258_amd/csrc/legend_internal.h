@@ -184,6 +184,81 @@ hipError_t launch_gather_rows(hipStream_t st, const int64_t* ids, int64_t m, flo
                               int32_t rows_per_partition, int64_t num_rows, int32_t dim, float* out,
                               uint32_t* err_flag);
 
+// ---- operators on the caller's tensors ------------------------------------------------------------
+inline bool type_known(int t) { return t >= LEGEND_TYPE_FLOAT && t <= LEGEND_TYPE_HALF; }
+inline int type_size(int t) { return t == LEGEND_TYPE_FLOAT ? 4 : 2; }
+
+// What they need of a context (runtime.hip keeps the struct to itself).
+struct CtxView {
+    int device = 0;
+    hipStream_t stream = nullptr;
+    int dim = 0, num_partitions = 0;
+    int64_t num_nodes = 0, rows_per_partition = 0;
+    int32_t relation_rows = 0;
+    float* const* part_emb = nullptr;       // device: embedding base per partition or null
+    const float* E_rel = nullptr;
+};
+int ctx_enter(legend_ctx* c, CtxView* v);            // usable context, its device made current
+int ctx_tables_current(legend_ctx* c, bool recording);   // the compute stream sees every finished and pending swap
+void ctx_failed(legend_ctx* c);                      // after a HIP error
+void ctx_keep(legend_ctx* c, legend_adamw* opt, bool attach);
+void adamw_orphan(legend_adamw* opt);                // its context is gone
+
+constexpr int kNormMaxDim = 1 << 20;
+struct NormParams {
+    int64_t rows;
+    int32_t dim;
+    float eps;
+    const void* x; int64_t x_stride; int32_t x_type;
+    // rows of a table instead: bases per partition (nodes) or one base (relations)
+    const int64_t* ids; float* const* part_base; const float* rel_base;
+    int64_t table_rows, rows_per_partition;
+    uint32_t* status;                       // null: x
+    const void* weight; const void* bias; int32_t weight_type;
+    float* mean; float* rstd;
+    void* y; int64_t y_stride; int32_t y_type;
+    const void* dy; int64_t dy_stride; int32_t dy_type;
+    void* dx; int64_t dx_stride;
+    void* dweight; void* dbias; int32_t dweight_type, accumulate;
+    float* partial;                         // [parts][2][dim]
+    int32_t parts;
+};
+int norm_parts(int64_t rows, int32_t dim);   // workgroups of the backward pass, each with partial sums of its own
+hipError_t launch_norm_forward(hipStream_t st, const NormParams& a);
+hipError_t launch_norm_backward(hipStream_t st, const NormParams& a);
+
+constexpr int kAdamBlock = 256;             // elements that share a scale
+constexpr int kAdamNormParts = 1024;        // partial sums of the gradient norm
+struct AdamTensor {
+    void* param; float* master; void* m; void* v; float* m_scale; float* v_scale;
+    int64_t count, first_unit;
+    double weight_decay, lr_scale;
+    int32_t param_type, grad_type, state_type, index;
+};
+struct AdamState {                          // device; what the next step needs besides the tensors
+    int64_t steps, skipped;
+    double inv_bias1;                       // 1 / (1 - beta1^t), t = steps + 1
+    float inv_bias2_root;                   // 1 / sqrt(1 - beta2^t)
+    uint32_t ticket;                        // workgroups of the running step that are done
+    uint64_t key;                           // fold(seed, t)
+};
+struct AdamParams {
+    const AdamTensor* tensors;
+    const void* const* grads;
+    const int32_t* unit_tensor;             // tensor of every unit
+    int64_t units;
+    int32_t unit_elems;                     // a multiple of kAdamBlock
+    AdamState* state;
+    double* partial;                        // [kAdamNormParts]
+    const float* grad_scale; const float* lr_factor; float* norm_out;
+    double lr, beta1, beta2, eps, max_norm;
+    uint64_t seed;
+    int32_t with_norm;
+};
+int adam_unit_elems(int64_t total);
+void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2, uint64_t seed);
+hipError_t launch_adamw(hipStream_t st, const AdamParams& a);
+
 int64_t update_long_rows_capacity(int64_t n_occ);
 int64_t update_long_units_capacity(int64_t n_occ);
 int row_tiles_for(int chunk_size, int dim);          // T

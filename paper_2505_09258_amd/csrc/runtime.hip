@@ -17,6 +17,7 @@
 #include "legend_internal.h"
 #include "device_utils.h"
 #include "host_copy.h"
+#include "host_guard.h"
 
 using namespace legend;
 
@@ -26,29 +27,6 @@ namespace {
 
 // message of the calling thread's last failure: a fixed buffer, so that reporting an error never allocates
 thread_local char g_last_error[512] = "";
-
-int fail(int code, const char* fmt, ...) noexcept {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
-    va_end(ap);
-    return code;
-}
-
-// Every entry point runs its body through this: no C++ exception (the containers of the host runtime
-// can throw std::bad_alloc) leaves the library through the C ABI.
-template <class F>
-int guarded(const char* what, F&& body) noexcept {
-    try {
-        return body();
-    } catch (const std::bad_alloc&) {
-        return fail(LEGEND_E_NOMEM, "%s: out of host memory", what);
-    } catch (const std::exception& e) {
-        return fail(LEGEND_E_STATE, "%s: unexpected failure in the host runtime: %s", what, e.what());
-    } catch (...) {
-        return fail(LEGEND_E_STATE, "%s: unexpected failure in the host runtime", what);
-    }
-}
 
 // Scratch memory of legend_rank_edges_static: lives in the code object, one copy per device, until the
 // process ends.  In host code the array's name is only a handle for hipGetSymbolAddress: the device
@@ -65,6 +43,16 @@ struct ProfSpan {
 };
 
 }  // namespace
+
+namespace legend {
+int fail(int code, const char* fmt, ...) noexcept {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
+    va_end(ap);
+    return code;
+}
+}  // namespace legend
 
 // device address of `scratch` on the current device `dev`; resolved on first use per device
 static int resolve_static_scratch(int dev) {
@@ -139,6 +127,7 @@ struct legend_ctx {
     bool keep_loss = false;                 // epoch driver: do not reset the device loss sum per bucket
     bool part_tables_dirty = false;         // d_part_emb / d_part_state lag behind part_slot
     bool fatal = false;
+    std::vector<legend_adamw*> optimisers;  // created on this context and not destroyed
 };
 
 namespace {
@@ -320,6 +309,7 @@ int do_swap(legend_ctx* c, int evict, int load, bool fence_now, bool early_load 
 void free_ctx(legend_ctx* c) {
     if (!c) return;
     (void)hipSetDevice(c->cfg.device);
+    for (legend_adamw* o : c->optimisers) adamw_orphan(o);
     c->readback.release();                  // every read has waited for its copies
     if (c->compute) (void)hipStreamSynchronize(c->compute);
     if (c->copy) (void)hipStreamSynchronize(c->copy);
@@ -379,6 +369,51 @@ int check_ctx(legend_ctx* c) {
     if (hipSetDevice(c->cfg.device) != hipSuccess) return fail(LEGEND_E_HIP, "hipSetDevice(%d) failed", c->cfg.device);
     return LEGEND_OK;
 }
+
+}  // namespace
+
+namespace legend {
+
+int ctx_enter(legend_ctx* c, CtxView* v) {
+    int rc = check_ctx(c);
+    if (rc) return rc;
+    v->device = c->cfg.device;
+    v->stream = c->compute;
+    v->dim = c->d;
+    v->num_partitions = c->n;
+    v->num_nodes = c->V;
+    v->rows_per_partition = c->Rp;
+    v->relation_rows = c->nrel_rows;
+    v->part_emb = c->d_part_emb;
+    v->E_rel = c->E_rel;
+    return LEGEND_OK;
+}
+
+int ctx_tables_current(legend_ctx* c, bool recording) {
+    if (recording) {
+        // neither the wait for a copy outside the recording nor the copy of the partition table can be recorded
+        bool pending = c->part_tables_dirty;
+        for (int s = 0; s < c->nslots; ++s) pending = pending || c->slot_pending[s];
+        if (pending) return fail(LEGEND_E_STATE, "a partition swap has not been seen by the compute stream yet: make one call outside the recording first");
+        return LEGEND_OK;
+    }
+    for (int s = 0; s < c->nslots; ++s) {
+        int rc = wait_slot(c, s);
+        if (rc) return rc;
+    }
+    return c->part_tables_dirty ? upload_part_tables(c) : LEGEND_OK;
+}
+
+void ctx_failed(legend_ctx* c) { c->fatal = true; }
+
+void ctx_keep(legend_ctx* c, legend_adamw* opt, bool attach) {
+    if (attach) c->optimisers.push_back(opt);
+    else c->optimisers.erase(std::remove(c->optimisers.begin(), c->optimisers.end(), opt), c->optimisers.end());
+}
+
+}  // namespace legend
+
+namespace {
 
 // Stage a bucket's edges on the device if they are in host memory; validate ids.
 int stage_edges(legend_ctx* c, int i, int j, const int32_t* edges, int64_t m, int mem, const int32_t** dev_out) {

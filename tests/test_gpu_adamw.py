@@ -1,0 +1,495 @@
+"""AdamW over many tensors against the 64-bit oracle.
+
+Tolerances count roundings, E = 2^-24 each (half a step of fp32).  With s = grad_scale * clip (3 roundings from the norm on):
+  g s: 4 E;  m: each term at most 6 E of itself;  v: (1 - beta2) g s g s: 10 E;  the constants 1 - beta, lr' / (1 - beta1^t): E each
+  root: half of v's + E;  root c + eps: + 3 E;  m / that: + 2 E;  the step: + 3 E: at most 22 E of |m terms| / denominator * rate
+  p: three roundings of the operands, then half a step of its type.
+8-bit states: a code is floor(x / step + u) steps; where x / step + u is nearer to a whole number than the errors of m (7 E of its
+terms) or of sqrt(v) (8 E) and of the scale, the fp32 value may fall on its other side, and nothing is asked of that code."""
+
+import numpy as np
+import pytest
+
+from oracle import dense as od
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0**-24
+HALF_STEP = {0: 2.0**-24, 1: 2.0**-8, 2: 2.0**-11}
+TINY = {0: 2.0**-149, 1: 2.0**-134, 2: 2.0**-25}
+HYPER = dict(beta1=0.9, beta2=0.999, eps=1e-8)
+CODES = od.e4m3_values()
+
+
+def _torch_type(k):
+    import torch
+    return (torch.float32, torch.bfloat16, torch.float16)[k]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2505_09258_amd import binding as L
+    cfg = L.make_config(num_nodes=3, dim=4, batch_size=64, chunk_size=16, num_negs=16, init_std=0.1, seed=1)
+    c = L.legend_init_partitions(cfg, None, None)
+    yield c
+    L.legend_destroy(c)
+
+
+def guarded(values, dtype, shift=0):
+    """A view of `values` inside an allocation with 8 guard elements behind it (and shift before it)."""
+    import torch
+    a = np.asarray(values)
+    flat = torch.full((shift + a.size + 8,), 77, dtype=dtype, device="cuda") if dtype == torch.uint8 else torch.full((shift + a.size + 8,), -77.0, dtype=dtype, device="cuda")
+    view = flat[shift:shift + a.size]
+    if a.size:
+        view.copy_(torch.from_numpy(np.ascontiguousarray(a)).to(dtype))
+    return flat, view, shift
+
+
+def guards_kept(g):
+    flat, view, shift = g
+    rest = [flat[:shift], flat[shift + view.numel():]]
+    mark = 77 if flat.dtype.is_floating_point is False else -77.0
+    return all(bool((r == mark).all()) for r in rest)
+
+
+class Tensor:
+    def __init__(self, count, pt=0, gt=0, block=False, master=False, decay=0.01, lr_scale=1.0, shift=0, seed=0, zero_state=False):
+        import torch
+        self.count, self.pt, self.gt, self.block, self.decay, self.lr_scale = count, pt, gt, block, decay, lr_scale
+        rng = np.random.default_rng(count + 17 * seed + pt)
+        size = np.exp(rng.standard_normal(count))
+        self.param = guarded(rng.standard_normal(count) * 0.1, _torch_type(pt), shift)
+        self.grad = guarded(rng.standard_normal(count) * size * 0.02, _torch_type(gt), shift)
+        self.master = guarded(self.param[1].double().cpu().numpy() * (1 + 1e-4), torch.float32, shift) if master else None
+        m, root = rng.standard_normal(count) * size * 4e-3, size * 2e-2
+        if zero_state:
+            m, root = 0 * m, 0 * root
+        if block:
+            self.m_scale, self.v_scale = (guarded(od.block_scales(a).astype(np.float32), torch.float32, 1) for a in (m, root))
+            self.m, self.v = (guarded(self.nearest(a, s), torch.uint8, shift) for a, s in ((m, self.m_scale), (root, self.v_scale)))
+        else:
+            self.m, self.v = guarded(m, torch.float32, shift), guarded(root * root, torch.float32, shift)
+
+    @staticmethod
+    def nearest(x, scale):
+        import torch
+        s = np.repeat(scale[1].double().cpu().numpy(), od.BLOCK)[: len(x)]
+        q = np.clip(np.where(s > 0, x / np.where(s > 0, s, 1), 0), -448, 448)
+        return torch.from_numpy(q.astype(np.float32)).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+
+    def parts(self):
+        return [self.param, self.grad, self.m, self.v] + ([self.master] if self.master else []) + ([self.m_scale, self.v_scale] if self.block else [])
+
+    def describe(self, **change):
+        from paper_2505_09258_amd import binding as L
+        p = lambda g: None if g is None else g[1].data_ptr()  # noqa: E731
+        a = dict(count=self.count, param=p(self.param), grad=p(self.grad), m=p(self.m), v=p(self.v), master=p(self.master), param_type=self.pt,
+                 grad_type=self.gt, state_type=int(self.block), weight_decay=self.decay, lr_scale=self.lr_scale)
+        if self.block:
+            a.update(m_scale=p(self.m_scale), v_scale=p(self.v_scale))
+        a.update(change)
+        return L.make_adamw_tensor(**a)
+
+    def numbers(self):
+        """(p, g, m, v, code of m, code of sqrt(v), scales) in 64 bits."""
+        n = lambda g: g[1].double().cpu().numpy()  # noqa: E731
+        p, g = n(self.master or self.param), n(self.grad)
+        if not self.block:
+            return dict(p=p, g=g, m=n(self.m), v=n(self.v))
+        cm, cr = (t[1].cpu().numpy() for t in (self.m, self.v))
+        sm, sr = n(self.m_scale), n(self.v_scale)
+        m, r = (CODES[c] * np.repeat(s, od.BLOCK)[: self.count] for c, s in ((cm, sm), (cr, sr)))
+        return dict(p=p, g=g, m=m, v=r * r, cm=cm, cr=cr, sm=sm, sr=sr)
+
+    def bytes(self):
+        return [t[1].clone() for t in self.parts() if t is not self.grad]
+
+
+def check_codes(codes, scales, x, word_share, least, err):
+    """x: the values in 64 bits, err: how far the fp32 ones may be from them."""
+    want = od.block_scales(x)
+    pad = np.pad(err, (0, -len(err) % od.BLOCK)).reshape(-1, od.BLOCK).max(1)
+    assert np.all(np.abs(scales - want) <= pad / 448 + 4 * E * want)
+    low, step, share = od.rounded_up_share(x, want, least)
+    unit = np.repeat(want, od.BLOCK)[: len(x)] * step
+    # in steps: the value's own error, and that of the scale, its reciprocal and the product (16 steps at most: 16 * 16 E)
+    loose = (err + np.repeat(pad, od.BLOCK)[: len(x)] * np.minimum(np.abs(x) / np.maximum(448 * np.repeat(want, od.BLOCK)[: len(x)], 1e-300), 1)) / np.maximum(unit, 1e-300) + 256 * E
+    sure = (np.abs(share + word_share - 1.0) > loose) & (np.minimum(share, 1 - share) > loose)
+    value = np.minimum(np.where(share + word_share >= 1.0, low + step, low), 448.0)
+    # a value within its errors of a code takes that code, whichever side it is on, unless the fraction drawn is as small (as near to 1)
+    beside = (np.minimum(share, 1 - share) <= loose) & (word_share > 2 * loose) & (word_share < 1 - 2 * loose)
+    value = np.where(beside, np.minimum(np.where(share < 0.5, low, low + step), 448.0), value)
+    sure |= beside | (np.abs(x) == 0)
+    got = CODES[codes]
+    assert np.array_equal(np.abs(got)[sure], value[sure])
+    assert np.array_equal(np.signbit(got)[sure & (value > 0)], np.signbit(x)[sure & (value > 0)])
+    # elsewhere it is one of the two codes around, or the one below
+    assert np.all((np.abs(got) >= low - step) & (np.abs(got) <= low + step))
+    assert len(x) < 300 or sure.mean() > 0.95
+
+
+def check_step(t, before, t_now, k, scale, lr, seed, hyper=HYPER):
+    """Tensor t after step t_now, from its numbers before; scale = grad_scale * clip in 64 bits."""
+    lr = lr * t.lr_scale
+    g = before["g"] * scale
+    p, m, v = od.adamw(before["p"], g, before["m"], before["v"], t_now, lr=lr, weight_decay=t.decay, **hyper)
+    after = t.numbers()
+    b1, b2, eps = hyper["beta1"], hyper["beta2"], hyper["eps"]
+    m_terms = b1 * np.abs(before["m"]) + (1 - b1) * np.abs(g)
+    if not t.block:
+        assert np.all(np.abs(after["m"] - m) <= 7 * E * m_terms + 2.0**-149)
+        assert np.all(np.abs(after["v"] - v) <= 12 * E * v + 2.0**-149)
+    den = np.sqrt(v / (1 - b2**t_now)) + eps
+    step = lr / (1 - b1**t_now) * m_terms / den
+    tol = 24 * E * step + 3 * E * (np.abs(before["p"]) + np.abs(p)) + 2.0**-149
+    got = after["p"]
+    if t.master is None:
+        tol = tol + HALF_STEP[t.pt] * np.abs(p) * (1 + 1e-3) + TINY[t.pt]
+    err = np.abs(got - p)
+    assert np.all(err <= tol), float((err / tol).max())
+    if t.master is not None:
+        import torch
+        assert torch.equal(t.param[1], t.master[1].to(t.param[1].dtype))
+    if t.block:
+        w = od.random_words(seed, t_now, k, t.count)
+        check_codes(after["cm"], after["sm"], m, (w >> np.uint64(12)) / 2.0**20, False, 7 * E * m_terms)
+        check_codes(after["cr"], after["sr"], np.sqrt(v), (w & np.uint64(0xFFFF)) / 2.0**16, True, 8 * E * np.sqrt(v))
+    assert all(guards_kept(x) for x in t.parts())
+
+
+def run_steps(ctx, tensors, steps=2, lr=0.01, max_norm=0.0, seed=3, grad_scale=None, lr_factor=None, want_norm=False, hyper=HYPER, start=0):
+    import torch
+    from paper_2505_09258_amd import binding as L
+    opt = L.legend_adamw_create(ctx, [t.describe() for t in tensors], max_norm=max_norm, seed=seed, **hyper)
+    try:
+        if start:
+            L.legend_adamw_set_steps(opt, start)
+        gs = None if grad_scale is None else torch.tensor([grad_scale], device="cuda")
+        lf = None if lr_factor is None else torch.tensor([lr_factor], device="cuda")
+        norm = torch.full((1,), -77.0, device="cuda") if want_norm else None
+        for step in range(1, steps + 1):
+            before = [t.numbers() for t in tensors]
+            torch.cuda.synchronize()
+            L.legend_adamw_step(opt, lr, *[None if s is None else s.data_ptr() for s in (lf, gs, norm)])
+            L.legend_sync(ctx)
+            s = 1.0 if gs is None else float(gs.double())
+            size = od.gradient_norm([b["g"] for b in before], s)
+            if want_norm:
+                assert abs(float(norm) - size) <= 2 * E * size
+            for k, t in enumerate(tensors):
+                check_step(t, before[k], start + step, k, s * od.clip_factor(size, max_norm), lr * (1.0 if lf is None else float(lf.double())), seed, hyper)
+        assert L.legend_adamw_get_steps(opt) == (start + steps, 0)
+    finally:
+        L.legend_adamw_destroy(opt)
+
+
+COUNTS = [1, 2, 3, 5, 63, 64, 65, 255, 256, 257, 511, 1_000, 1_023, 1_024, 1_025, 4_095, 4_096, 4_097, 10_007, 70_001]
+
+
+@pytest.mark.parametrize("block", [False, True], ids=["float", "block"])
+@pytest.mark.parametrize("count", COUNTS, ids=str)
+def test_one_tensor(ctx, count, block):
+    run_steps(ctx, [Tensor(count, block=block)])
+
+
+@pytest.mark.parametrize("block", [False, True], ids=["float", "block"])
+@pytest.mark.parametrize("pt,gt,master", [(0, 0, False), (0, 1, False), (0, 2, False), (1, 1, False), (1, 1, True), (1, 0, True), (1, 2, True), (2, 2, False), (2, 2, True),
+                                          (2, 0, False), (2, 1, True)], ids=lambda v: str(v))
+@pytest.mark.parametrize("shift", [0, 1, 3], ids=["s0", "s1", "s3"])
+def test_types_at_odd_addresses(ctx, pt, gt, master, block, shift):
+    run_steps(ctx, [Tensor(2_900, pt, gt, block, master, shift=shift)], max_norm=0.5, want_norm=True)
+
+
+@pytest.mark.parametrize("max_norm", [0.0, 0.3, 1e6], ids=["free", "clipped", "loose"])
+def test_many_tensors_of_all_kinds(ctx, max_norm):
+    rng = np.random.default_rng(4)
+    tensors = []
+    for k in range(60):
+        pt = int(rng.integers(0, 3))
+        tensors.append(Tensor(int(rng.choice([0, 1, 7, 100, 256, 300, 1_025, 5_000, 20_000])), pt, int(rng.choice([0, pt])), bool(rng.integers(0, 2)),
+                              pt > 0 and bool(rng.integers(0, 2)), decay=float(rng.choice([0.0, 0.1])), lr_scale=float(rng.choice([0.0, 0.5, 1.0])),
+                              shift=int(rng.integers(0, 4)), seed=k))
+    run_steps(ctx, tensors, steps=3, max_norm=max_norm, grad_scale=0.25, lr_factor=0.5, want_norm=max_norm > 1)
+
+
+@pytest.mark.parametrize("block", [False, True], ids=["float", "block"])
+def test_many_units(ctx, block):
+    """More units than workgroups, the last ones partial."""
+    run_steps(ctx, [Tensor(3_000_017, block=block), Tensor(5, block=block), Tensor(9_000_001, 1, 1, block, True, shift=1)], steps=1, max_norm=1.0)
+
+
+@pytest.mark.parametrize("hyper", [dict(beta1=0.0, beta2=0.0, eps=1e-3), dict(beta1=0.5, beta2=0.9, eps=1e-6)], ids=["none", "short"])
+@pytest.mark.parametrize("start", [0, 12_345], ids=["first", "later"])
+def test_other_constants(ctx, hyper, start):
+    run_steps(ctx, [Tensor(1_500), Tensor(1_500, block=True)], hyper=hyper, start=start)
+
+
+@pytest.mark.parametrize("block", [False, True], ids=["float", "block"])
+def test_states_that_start_at_zero(ctx, block):
+    run_steps(ctx, [Tensor(3_000, block=block, zero_state=True)], steps=3)
+
+
+def test_zero_rate_changes_states_only(ctx):
+    t = Tensor(700)
+    p = t.param[1].clone()
+    run_steps(ctx, [t], lr=0.0, steps=1)
+    import torch
+    assert torch.equal(p, t.param[1])
+
+
+def test_zero_gradients(ctx):
+    import torch
+    a, b = Tensor(600, block=True, zero_state=True), Tensor(600, zero_state=True)
+    for t in (a, b):
+        t.grad[1].zero_()
+    run_steps(ctx, [a, b], max_norm=1.0, want_norm=True)
+    assert not bool(a.m[1].any()) and not bool(a.v[1].any()) and not bool(a.m_scale[1].any()) and not bool(b.v[1].any())
+    assert bool(torch.isfinite(a.param[1]).all())
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")], ids=["nan", "inf", "minus_inf"])
+def test_a_step_with_a_gradient_that_is_not_finite_is_skipped(ctx, value):
+    import torch
+    from paper_2505_09258_amd import binding as L
+    tensors = [Tensor(5_000), Tensor(3_000, 1, 1, True, True), Tensor(40)]
+    opt = L.legend_adamw_create(ctx, [t.describe() for t in tensors], max_norm=1.0, seed=1, **HYPER)
+    try:
+        keep = float(tensors[1].grad[1][2_999])
+        tensors[1].grad[1][2_999] = value
+        before = [t.bytes() for t in tensors]
+        norm = torch.zeros(1, device="cuda")
+        torch.cuda.synchronize()
+        L.legend_adamw_step(opt, 0.01, norm=norm.data_ptr())
+        L.legend_adamw_step(opt, 0.01)
+        L.legend_sync(ctx)
+        assert not bool(torch.isfinite(norm))
+        assert all(torch.equal(x, y) for t, b in zip(tensors, before) for x, y in zip(t.bytes(), b))
+        assert L.legend_adamw_get_steps(opt) == (0, 2)
+        tensors[1].grad[1][2_999] = keep
+        numbers = [t.numbers() for t in tensors]
+        torch.cuda.synchronize()
+        L.legend_adamw_step(opt, 0.01)
+        L.legend_sync(ctx)
+        assert L.legend_adamw_get_steps(opt) == (1, 2)
+        f = od.clip_factor(od.gradient_norm([n["g"] for n in numbers]), 1.0)
+        for k, t in enumerate(tensors):
+            check_step(t, numbers[k], 1, k, f, 0.01, 1)
+    finally:
+        L.legend_adamw_destroy(opt)
+
+
+def test_without_a_norm_such_a_gradient_stays_with_its_element(ctx):
+    import torch
+    from paper_2505_09258_amd import binding as L
+    tensors = [Tensor(600), Tensor(600, block=True)]
+    clean = [Tensor(600), Tensor(600, block=True)]
+    for t in tensors:
+        t.grad[1][77], t.grad[1][300] = float("nan"), float("inf")
+    for ts in (tensors, clean):
+        opt = L.legend_adamw_create(ctx, [t.describe() for t in ts], seed=1, **HYPER)
+        torch.cuda.synchronize()
+        L.legend_adamw_step(opt, 0.01)
+        L.legend_adamw_destroy(opt)
+    fine = torch.ones(600, dtype=torch.bool, device="cuda")
+    fine[[77, 300]] = False
+    for t, c in zip(tensors, clean):
+        assert torch.equal(t.param[1][fine], c.param[1][fine])
+        assert bool(t.param[1][~fine].isnan().all())
+    codes = tensors[1].m[1].cpu().numpy()
+    assert np.isnan(CODES[codes[[77, 300]]]).all() and np.isfinite(CODES[codes[fine.cpu().numpy()]]).all()
+    assert np.isnan(CODES[tensors[1].v[1].cpu().numpy()[[77, 300]]]).all()
+    assert bool(torch.isfinite(tensors[1].m_scale[1]).all()) and bool(torch.isfinite(tensors[1].v_scale[1]).all())
+    # the blocks' other elements are coded in units of the largest finite one
+    top = np.abs(CODES[codes[:256][fine.cpu().numpy()[:256]]]).max()
+    assert top == 448.0
+
+
+def test_other_gradients_and_steps(ctx):
+    import torch
+    from paper_2505_09258_amd import binding as L
+    t, other = Tensor(2_000, block=True), Tensor(2_000, seed=9)
+    opt = L.legend_adamw_create(ctx, [t.describe()], seed=5, **HYPER)
+    try:
+        L.legend_adamw_set_gradients(opt, [other.grad[1].data_ptr()])
+        L.legend_adamw_set_steps(opt, 99)
+        before = t.numbers()
+        before["g"] = other.grad[1].double().cpu().numpy()
+        torch.cuda.synchronize()
+        L.legend_adamw_step(opt, 0.01)
+        L.legend_sync(ctx)
+        check_step(t, before, 100, 0, 1.0, 0.01, 5)
+        assert L.legend_adamw_get_steps(opt) == (100, 0)
+    finally:
+        L.legend_adamw_destroy(opt)
+
+
+def test_the_same_bits_again(ctx):
+    import torch
+    from paper_2505_09258_amd import binding as L
+    runs = []
+    for _ in range(2):
+        ts = [Tensor(100_003, 1, 1, True, True), Tensor(33_000, seed=2), Tensor(70, 2, 2)]
+        opt = L.legend_adamw_create(ctx, [t.describe() for t in ts], max_norm=0.7, seed=8, **HYPER)
+        torch.cuda.synchronize()
+        for _ in range(5):
+            L.legend_adamw_step(opt, 0.01)
+        L.legend_adamw_destroy(opt)                                   # waits
+        runs.append([x for t in ts for x in t.bytes()])
+    assert all(torch.equal(x, y) for x, y in zip(*runs))
+
+
+def test_replayed_graph_is_the_next_step():
+    import torch
+    from paper_2505_09258_amd import binding as L
+    stream = torch.cuda.Stream()
+    cfg = L.make_config(num_nodes=3, dim=4, batch_size=64, chunk_size=16, num_negs=16, init_std=0.1, seed=1, compute_stream=stream.cuda_stream)
+    c = L.legend_init_partitions(cfg, None, None)
+    try:
+        with torch.cuda.stream(stream):
+            sets = [[Tensor(10_000, 1, 1, True, True), Tensor(999, seed=3)] for _ in range(2)]
+            opts = [L.legend_adamw_create(c, [t.describe() for t in ts], max_norm=0.5, seed=2, **HYPER) for ts in sets]
+            factor, norm = torch.ones(1, device="cuda"), torch.zeros(1, device="cuda")
+            stream.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                L.legend_adamw_step(opts[0], 0.02, lr_factor=factor.data_ptr(), norm=norm.data_ptr())
+            assert L.legend_adamw_get_steps(opts[0]) == (0, 0)
+            for turn in range(1, 6):
+                factor.fill_(1.0 / turn)
+                for ts in sets:
+                    for k, t in enumerate(ts):
+                        g = torch.Generator(device="cuda")
+                        g.manual_seed(10 * turn + k)
+                        t.grad[1].copy_(torch.randn(t.count, generator=g, device="cuda") * 0.01)
+                if turn == 3:                                        # an eager step between replays is a step like any other
+                    L.legend_adamw_step(opts[0], 0.02, lr_factor=factor.data_ptr())
+                else:
+                    graph.replay()
+                L.legend_adamw_step(opts[1], 0.02, lr_factor=factor.data_ptr())
+                torch.cuda.synchronize()
+                for t, u in zip(*sets):
+                    assert all(torch.equal(x, y) for x, y in zip(t.bytes(), u.bytes())), turn
+                assert L.legend_adamw_get_steps(opts[0]) == (turn, 0)
+            for o in opts:
+                L.legend_adamw_destroy(o)
+    finally:
+        L.legend_destroy(c)
+
+
+def test_codes_follow_on_average(ctx):
+    """sqrt(v) of a constant gradient, from twice its size: each step takes 0.05 % off, a code is 6 to 12 %.  Rounded to nearest
+    it would stay where it is.  Rounding up or down by chance leaves sqrt(v) a spread of at most a quarter around the exact value (codes of
+    an eighth, one change in 2 / 0.001 steps remembered: 0.125 sqrt(0.0005 / 0.125 / 0.001) = 0.25), whose effect on the mean over all elements
+    through the curvature of the square root is at most half its square, 3 %; the mean over 50 000 elements itself moves by 0.1 %."""
+    import torch
+    from paper_2505_09258_amd import binding as L
+    n = 200 * 256
+    t = Tensor(n, block=True)
+    rng = np.random.default_rng(0)
+    g = np.exp2(-5 * rng.random(n)).astype(np.float32) * rng.choice([-1, 1], n)
+    t.grad[1].copy_(torch.from_numpy(g))
+    root = 2.0 * np.abs(g)
+    s = od.block_scales(root).astype(np.float32)
+    t.v_scale[1].copy_(torch.from_numpy(s))
+    t.v[1].copy_(torch.from_numpy(Tensor.nearest(root, t.v_scale)))
+    t.m[1].zero_()
+    t.m_scale[1].zero_()
+    start = np.mean(np.sqrt(t.numbers()["v"]) / np.abs(g))
+    opt = L.legend_adamw_create(ctx, [t.describe()], seed=77, **HYPER)
+    torch.cuda.synchronize()
+    for _ in range(1_500):
+        L.legend_adamw_step(opt, 0.0)
+    L.legend_adamw_destroy(opt)
+    after = t.numbers()
+    want = np.sqrt(4 * 0.999**1_500 + (1 - 0.999**1_500))
+    got = np.mean(np.sqrt(after["v"]) / np.abs(g))
+    assert abs(start - 2.0) < 0.01 and abs(got - want) < 0.05 * want, (got, want)
+    assert abs(np.mean(after["m"] / g) - 1.0) < 0.01
+
+
+def test_head_over_the_table_learns_in_a_graph():
+    """The operators as a program uses them: rows of the table, normalised, times a weight; the gradients of all of it; one step.
+    Every replay is compared with the same chain in 64 bits, from the weights that the replay before it left."""
+    import torch
+    from paper_2505_09258_amd import binding as L
+    rng = np.random.default_rng(6)
+    V, d, rows, out = 2_000, 100, 300, 16
+    node = rng.standard_normal((V, d)).astype(np.float32)
+    stream = torch.cuda.Stream()
+    cfg = L.make_config(num_nodes=V, dim=d, batch_size=64, chunk_size=16, num_negs=16, seed=1, compute_stream=stream.cuda_stream)
+    c = L.legend_init_partitions(cfg, node, None)
+    try:
+        L.legend_swap_partition(c, -1, 0)
+        with torch.cuda.stream(stream):
+            ids = torch.from_numpy(rng.integers(0, V, rows)).cuda()
+            target = torch.from_numpy(rng.standard_normal((rows, out)).astype(np.float32)).cuda()
+            f = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+            w, b, proj = torch.ones(d, device="cuda"), f(d), torch.from_numpy((rng.standard_normal((d, out)) * 0.1).astype(np.float32)).cuda()
+            dw, db, dproj = f(d), f(d), f(d, out)
+            y, mean, rstd, dy, dx, status = f(rows, d), f(rows), f(rows), f(rows, d), f(rows, d), torch.zeros(1, dtype=torch.int32, device="cuda")
+            size = L.legend_layer_norm_workspace(rows, d)
+            space, norm = f(size // 4), f(1)
+            a = L.make_layer_norm(rows=rows, dim=d, table=L.TABLE_NODE_EMB, ids=ids.data_ptr(), status=status.data_ptr(), weight=w.data_ptr(), bias=b.data_ptr(),
+                                  mean=mean.data_ptr(), rstd=rstd.data_ptr(), y=y.data_ptr(), dy=dy.data_ptr(), dx=dx.data_ptr(), dweight=dw.data_ptr(),
+                                  dbias=db.data_ptr(), workspace=space.data_ptr(), workspace_bytes=size)
+            states = [(f(t.numel()), f(t.numel())) for t in (w, b, proj)]
+            opt = L.legend_adamw_create(c, [L.make_adamw_tensor(count=t.numel(), param=t.data_ptr(), grad=g.data_ptr(), m=m.data_ptr(), v=v.data_ptr(), weight_decay=wd)
+                                            for t, g, (m, v), wd in zip((w, b, proj), (dw, db, dproj), states, (0.0, 0.0, 0.01))], max_norm=1.0, **HYPER)
+
+            def step():
+                L.legend_layer_norm_forward(c, a)
+                e = (y @ proj - target) * (2.0 / rows)
+                torch.mm(y.t(), e, out=dproj)
+                torch.mm(e, proj.t(), out=dy)
+                L.legend_layer_norm_backward(c, a)
+                L.legend_adamw_step(opt, 0.01, norm=norm.data_ptr())
+
+            step()                                                   # warms the library up, and lets the swap be seen
+            stream.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                step()
+            x64 = node[ids.cpu().numpy()].astype(np.float64)
+            for turn in range(2, 6):
+                before = [t.double().cpu().numpy() for t in (w, b, proj)]
+                sb = [(m.double().cpu().numpy(), v.double().cpu().numpy()) for m, v in states]
+                torch.cuda.synchronize()
+                graph.replay()
+                torch.cuda.synchronize()
+                y64, m64, r64 = od.layer_norm(x64, before[0], before[1], 1e-5)
+                e64 = (y64 @ before[2] - target.double().cpu().numpy()) * (2.0 / rows)
+                dx64, dw64, db64 = od.layer_norm_backward(x64, e64 @ before[2].T, m64, r64, before[0])
+                grads = [dw64, db64, y64.T @ e64]
+                size64 = od.gradient_norm(grads)
+                assert float(norm) == pytest.approx(size64, rel=1e-5)
+                assert np.abs(dx.double().cpu().numpy() - dx64).max() <= 1e-5 * np.abs(dx64).max()
+                for t, p, g, (m, v), wd, shape in zip((w, b, proj), before, grads, sb, (0.0, 0.0, 0.01), ((d,), (d,), (d, out))):
+                    want, _, _ = od.adamw(p.reshape(-1), g.reshape(-1) * od.clip_factor(size64, 1.0), m, v, turn, lr=0.01, weight_decay=wd, **HYPER)
+                    # a relative error r of a gradient moves a step of at most 3.2 lr (m / sqrt(v) of these constants) by 2 r of itself
+                    assert np.abs(t.double().cpu().numpy().reshape(-1) - want).max() <= 0.01 * 3.2 * 2 * 1e-3
+            assert int(status[0]) == 0 and L.legend_adamw_get_steps(opt) == (5, 0)
+            L.legend_adamw_destroy(opt)
+    finally:
+        L.legend_destroy(c)
+
+
+def test_real_refusals(ctx):
+    """The checks that the CPU tests go through, once on the library itself: nothing runs, and the optimiser is as it was."""
+    import torch
+    from paper_2505_09258_amd import binding as L
+    t = Tensor(300)
+    with pytest.raises(L.LegendError) as e:
+        L.legend_adamw_create(ctx, [t.describe(), t.describe()])
+    assert e.value.code == L.LEGEND_E_INVAL and "overlaps" in str(e.value)
+    with pytest.raises(L.LegendError):
+        L.legend_layer_norm_forward(ctx, L.make_layer_norm(rows=2, dim=0, x=t.param[1].data_ptr(), y=t.m[1].data_ptr()))
+    cfg = L.make_config(num_nodes=3, dim=4, batch_size=64, chunk_size=16, num_negs=16, init_std=0.1, seed=1)
+    c = L.legend_init_partitions(cfg, None, None)
+    opt = L.legend_adamw_create(c, [t.describe()])
+    L.legend_destroy(c)
+    with pytest.raises(L.LegendError) as e:
+        L.legend_adamw_step(opt, 0.1)
+    assert e.value.code == L.LEGEND_E_STATE
+    L.legend_adamw_destroy(opt)
+    assert torch.cuda.current_device() == 0
