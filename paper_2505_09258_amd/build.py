@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(HERE, "liblegend_hip.so")
 
 SOURCES = ["runtime.hip", "kernels_prepare.hip", "kernels_sort.hip", "kernels_chunk.hip", "kernels_chunk_gemm.hip", "kernels_chunk_split.hip",
            "kernels_update.hip", "kernels_rank.hip", "kernels_chunk_trans.hip", "order_plan.cpp", "dense.hip",
-           "kernels_norm.hip", "kernels_adamw.hip"]
+           "kernels_norm.hip", "kernels_norm_backward.hip", "kernels_adamw.hip"]
 # translation units of one source with one value of a macro each: source, macro, values
 VARIANTS = [("kernels_chunk_split.hip", "LEGEND_SPLIT_NJ", (2, 4, 6, 7, 8))]
 

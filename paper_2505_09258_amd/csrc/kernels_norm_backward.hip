@@ -1,0 +1,190 @@
+// Layer norm, backward: the gradient of the rows, and the sums over rows that the weight's and the bias's gradients are.
+//
+//   xh = (x - mean) rstd,  u = dy w,  dx = rstd (u - mean(u) - xh mean(u xh)),  dw = sum_rows dy xh,  db = sum_rows dy
+//
+// A row's x and dy stay in the registers of 8 to 1024 threads.  A thread keeps the same columns from row to row and adds up its
+// columns' dw and db; a workgroup writes its sums once, and a second kernel adds those in 64 bits, in a fixed order (no
+// atomics: the same bits every time).  Bound by HBM.
+#include "norm_rows.h"
+
+namespace legend {
+
+template <class XT, class YT, class S>
+__global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
+    constexpr int NE = S::NE, T = S::T, R = S::R, G = S::groups;
+    __shared__ float box[2][32];
+    __shared__ float sums[G > 1 ? 2 * 256 * NE : 1];
+    int turn = 0;
+    const int d = a.dim, lane = threadIdx.x % T;
+    const bool quads = (d & 3) == 0;
+    const int64_t groups = (int64_t)gridDim.x * G;
+    float w[NE], dw[NE], db[NE];
+    load_parameter<NE, T>(a.weight, a.weight_type, 1.f, d, lane, quads, w);
+#pragma unroll
+    for (int k = 0; k < NE; ++k) dw[k] = db[k] = 0.f;
+    for (int64_t r0 = ((int64_t)blockIdx.x * G + threadIdx.x / T) * R; r0 < a.rows; r0 += groups * R) {
+        float x[R][NE], g[R][NE], mean[R], rstd[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const XT* src = r0 + i < a.rows ? source_row<XT>(a, r0 + i, lane == 0) : nullptr;
+            mean[i] = rstd[i] = 0.f;
+            if (src) {
+                load_columns<NE, T>(src, d, lane, quads, x[i]);
+                load_columns<NE, T>(static_cast<const YT*>(a.dy) + (r0 + i) * a.dy_stride, d, lane, quads, g[i]);
+                mean[i] = a.mean[r0 + i];
+                rstd[i] = a.rstd[r0 + i];
+            } else {
+#pragma unroll
+                for (int k = 0; k < NE; ++k) x[i][k] = g[i][k] = 0.f;      // nothing to add, a gradient of zeros
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if (r0 + i >= a.rows) continue;
+            float su = 0.f, sx = 0.f;
+#pragma unroll
+            for (int k = 0; k < NE; ++k) {
+                x[i][k] = column_of<NE, T>(k, lane, quads) < d ? (x[i][k] - mean[i]) * rstd[i] : 0.f;
+                dw[k] += g[i][k] * x[i][k];
+                db[k] += g[i][k];
+                g[i][k] *= w[k];
+                su += g[i][k];
+                sx += g[i][k] * x[i][k];
+            }
+            if (!a.dx) continue;
+            row_sum2<T>(su, sx, box, turn);
+            su /= (float)d;
+            sx /= (float)d;
+#pragma unroll
+            for (int k = 0; k < NE; ++k) g[i][k] = rstd[i] * (g[i][k] - su - x[i][k] * sx);
+            store_columns<NE, T>(static_cast<XT*>(a.dx) + (r0 + i) * a.dx_stride, d, lane, quads, g[i]);
+        }
+    }
+    if (!a.partial) return;
+    float* out = a.partial + (int64_t)blockIdx.x * 2 * d;
+    if (G == 1) {
+        store_columns<NE, T>(out, d, lane, quads, dw);
+        store_columns<NE, T>(out + d, d, lane, quads, db);
+        return;
+    }
+    float* mine = sums + (threadIdx.x / T) * (2 * T * NE);
+#pragma unroll
+    for (int k = 0; k < NE; ++k) {
+        mine[column_of<NE, T>(k, lane, quads)] = dw[k];
+        mine[T * NE + column_of<NE, T>(k, lane, quads)] = db[k];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * T * NE; c += S::threads) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < G; ++k) s += sums[k * (2 * T * NE) + c];
+        const int col = c < T * NE ? c : c - T * NE;
+        if (col < d) out[c < T * NE ? col : d + col] = s;
+    }
+}
+
+// ---- rows of any length ------------------------------------------------------------------------------------------------
+
+template <class XT, class YT>
+__global__ void __launch_bounds__(1024) k_norm_backward_long(NormParams a) {
+    __shared__ float box[2][32];
+    int turn = 0;
+    const int d = a.dim;
+    float* pw = a.partial + (int64_t)blockIdx.x * 2 * d;       // sums of this workgroup's rows
+    float* pb = pw + d;
+    bool first = true;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const XT* x = source_row<XT>(a, r, threadIdx.x == 0);
+        const YT* dy = static_cast<const YT*>(a.dy) + r * a.dy_stride;
+        XT* dx = a.dx ? static_cast<XT*>(a.dx) + r * a.dx_stride : nullptr;
+        if (!x) {
+            if (dx) for (int c = threadIdx.x; c < d; c += 1024) dx[c] = (XT)0.f;
+            continue;
+        }
+        const float mean = a.mean[r], rstd = a.rstd[r];
+        float su = 0.f, sx = 0.f;
+        for (int c = threadIdx.x; c < d; c += 1024) {
+            const float g = (float)dy[c], xh = ((float)x[c] - mean) * rstd;
+            const float u = a.weight ? g * load_as(a.weight, c, a.weight_type) : g;
+            su += u;
+            sx += u * xh;
+            if (a.partial) {
+                pw[c] = first ? g * xh : pw[c] + g * xh;
+                pb[c] = first ? g : pb[c] + g;
+            }
+        }
+        first = false;
+        if (!dx) continue;
+        row_sum2<1024>(su, sx, box, turn);
+        su /= (float)d;
+        sx /= (float)d;
+        for (int c = threadIdx.x; c < d; c += 1024) {
+            const float g = (float)dy[c], xh = ((float)x[c] - mean) * rstd;
+            const float u = a.weight ? g * load_as(a.weight, c, a.weight_type) : g;
+            dx[c] = (XT)(rstd * (u - su - xh * sx));
+        }
+    }
+    if (a.partial && first)
+        for (int c = threadIdx.x; c < d; c += 1024) pw[c] = pb[c] = 0.f;
+}
+
+// Sums of the workgroups' partial sums, in 64 bits: 32 columns a workgroup, each by 32 threads that take every 32nd part, added
+// in the order of the threads.
+__global__ void __launch_bounds__(1024) k_norm_sums(NormParams a) {
+    __shared__ double box[32][33];
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    const int64_t width = 2 * (int64_t)a.dim;
+    double s = 0.0;
+    if (c < width) {
+#pragma unroll 8
+        for (int p = slice; p < a.parts; p += 32) s += (double)a.partial[p * width + c];
+    }
+    box[slice][lane] = s;
+    __syncthreads();
+    if (slice || c >= width) return;
+    void* out = c < a.dim ? a.dweight : a.dbias;
+    if (!out) return;
+    const int64_t at = c < a.dim ? c : c - a.dim;
+    s = a.accumulate ? (double)load_as(out, at, a.dweight_type) : 0.0;
+    for (int k = 0; k < 32; ++k) s += box[k][lane];
+    store_as(out, at, a.dweight_type, (float)s);
+}
+
+// Workgroups of the backward pass.  With sums wanted, each writes 8 bytes a column, which the second kernel reads again: two a
+// compute unit are enough to keep loads in flight, and few enough that their sums stay a small share of what the rows take.
+int norm_parts(int64_t rows, int32_t dim) {
+    int64_t need = rows, most = 512;
+    if (dim <= kNormRowMax)
+        for_shape(dim, [&](auto s) {
+            typedef decltype(s) S;
+            need = (rows + S::groups * S::R - 1) / (S::groups * S::R);
+            return 0;
+        });
+    return (int)(need < most ? need : most);
+}
+
+hipError_t launch_norm_backward(hipStream_t st, const NormParams& a) {
+    if (a.rows > 0) {
+        hipError_t e = for_types(a.x_type, a.dy_type, [&](auto xt, auto yt) {
+            if (a.dim > kNormRowMax) {
+                k_norm_backward_long<decltype(xt), decltype(yt)><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
+            } else {
+                for_shape(a.dim, [&](auto s) {
+                    typedef decltype(s) S;
+                    const int64_t need = (a.rows + S::groups * S::R - 1) / (S::groups * S::R), most = 256 * 2048 / S::threads;
+                    const unsigned grid = a.partial ? (unsigned)a.parts : (unsigned)(need < most ? need : most);
+                    k_norm_backward<decltype(xt), decltype(yt), S><<<grid, S::threads, 0, st>>>(a);
+                    return 0;
+                });
+            }
+            return hipGetLastError();
+        });
+        if (e != hipSuccess) return e;
+    }
+    if (!a.dweight && !a.dbias) return hipSuccess;
+    k_norm_sums<<<(unsigned)((2 * (int64_t)a.dim + 31) / 32), 1024, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace legend
