@@ -19,61 +19,70 @@ __global__ void __launch_bounds__(S::threads) k_norm_forward(NormParams a) {
     __shared__ float box[2][32];
     int turn = 0;
     const int d = a.dim, lane = threadIdx.x % T;
-    const bool quads = (d & 3) == 0;
-    const int64_t groups = (int64_t)gridDim.x * S::groups;
+    const float inv_d = 1.f / (float)d;
+    const int64_t stride = (int64_t)gridDim.x * S::groups * R;
+    RowColumns<XT, S> next[R];
+    bool next_good[R];
+    auto load = [&](int64_t r0) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const XT* src = r0 + i < a.rows ? source_row<XT>(a, r0 + i, lane == 0) : nullptr;
+            next_good[i] = src != nullptr;
+            if (src) next[i].load(src, d, lane);
+            else next[i].clear();
+        }
+    };
+    int64_t r0 = ((int64_t)blockIdx.x * S::groups + threadIdx.x / T) * R;
+    load(r0);
     float w[NE], b[NE];
-    load_parameter<NE, T>(a.weight, a.weight_type, 1.f, d, lane, quads, w);
-    load_parameter<NE, T>(a.bias, a.weight_type, 0.f, d, lane, quads, b);
-    for (int64_t r0 = ((int64_t)blockIdx.x * S::groups + threadIdx.x / T) * R; r0 < a.rows; r0 += groups * R) {
+    load_parameter<S>(a.weight, a.weight_type, 1.f, d, lane, w);
+    load_parameter<S>(a.bias, a.weight_type, 0.f, d, lane, b);
+    for (; r0 < a.rows; r0 += stride) {
         float x[R][NE];
         bool good[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const XT* src = r0 + i < a.rows ? source_row<XT>(a, r0 + i, lane == 0) : nullptr;
-            good[i] = src != nullptr;
-            if (src) {
-                load_columns<NE, T>(src, d, lane, quads, x[i]);
-            } else {
+            good[i] = next_good[i];
 #pragma unroll
-                for (int k = 0; k < NE; ++k) x[i][k] = 0.f;
-            }
+            for (int k = 0; k < NE; ++k) x[i][k] = S::inside(k, lane, d) ? next[i].number(k) : 0.f;
         }
+        if (r0 + stride < a.rows) load(r0 + stride);          // the next rows arrive while these are worked on
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             if (r0 + i >= a.rows) continue;
             float sum = 0.f, none = 0.f;
 #pragma unroll
             for (int k = 0; k < NE; ++k) sum += x[i][k];
-            row_sum2<T>(sum, none, box, turn);
-            const float mean = sum / (float)d;
+            row_sum<T, 1>(sum, none, box, turn);
+            const float mean = sum * inv_d;
             float left = 0.f, sq = 0.f;
 #pragma unroll
             for (int k = 0; k < NE; ++k) {
-                x[i][k] = column_of<NE, T>(k, lane, quads) < d ? x[i][k] - mean : 0.f;
+                x[i][k] = S::inside(k, lane, d) ? x[i][k] - mean : 0.f;
                 left += x[i][k];
-                sq += x[i][k] * x[i][k];
+                sq = fmaf(x[i][k], x[i][k], sq);
             }
-            row_sum2<T>(left, sq, box, turn);
-            left /= (float)d;
-            float var = sq / (float)d;
+            row_sum<T, 2>(left, sq, box, turn);
+            left *= inv_d;
+            float var = sq * inv_d;
             if (left * left > kLeftShare * var) {
                 sq = 0.f;
 #pragma unroll
                 for (int k = 0; k < NE; ++k) {
-                    const float v = column_of<NE, T>(k, lane, quads) < d ? x[i][k] - left : 0.f;
-                    sq += v * v;
+                    const float v = S::inside(k, lane, d) ? x[i][k] - left : 0.f;
+                    sq = fmaf(v, v, sq);
                 }
-                row_sum2<T>(sq, none, box, turn);
-                var = sq / (float)d;
+                row_sum<T, 1>(sq, none, box, turn);
+                var = sq * inv_d;
             } else {
-                var -= left * left;
+                var = fmaf(-left, left, var);
             }
-            const float rstd = good[i] ? 1.0f / sqrtf(var + a.eps) : 0.f;
+            const float rstd = good[i] ? 1.f / sqrtf(var + a.eps) : 0.f;
 #pragma unroll
-            for (int k = 0; k < NE; ++k) x[i][k] = good[i] ? (x[i][k] - left) * rstd * w[k] + b[k] : 0.f;
-            store_columns<NE, T>(static_cast<YT*>(a.y) + (r0 + i) * a.y_stride, d, lane, quads, x[i]);
+            for (int k = 0; k < NE; ++k) x[i][k] = good[i] ? fmaf((x[i][k] - left) * rstd, w[k], b[k]) : 0.f;
+            store_columns<S>(static_cast<YT*>(a.y) + (r0 + i) * a.y_stride, d, lane, x[i]);
             if (lane == 0) {
-                if (a.mean) a.mean[r0 + i] = mean + left;
+                if (a.mean) a.mean[r0 + i] = good[i] ? mean + left : 0.f;
                 if (a.rstd) a.rstd[r0 + i] = rstd;
             }
         }
@@ -93,7 +102,7 @@ __global__ void __launch_bounds__(1024) k_norm_forward_long(NormParams a) {
         float mean = 0.f, rstd = 0.f, left = 0.f, none = 0.f;
         if (x) {
             for (int c = threadIdx.x; c < d; c += 1024) mean += (float)x[c];
-            row_sum2<1024>(mean, none, box, turn);
+            row_sum<1024, 1>(mean, none, box, turn);
             mean /= (float)d;
             float sq = 0.f;
             for (int c = threadIdx.x; c < d; c += 1024) {
@@ -101,7 +110,7 @@ __global__ void __launch_bounds__(1024) k_norm_forward_long(NormParams a) {
                 left += v;
                 sq += v * v;
             }
-            row_sum2<1024>(left, sq, box, turn);
+            row_sum<1024, 2>(left, sq, box, turn);
             left /= (float)d;
             float var = sq / (float)d;
             if (left * left > kLeftShare * var) {
@@ -110,7 +119,7 @@ __global__ void __launch_bounds__(1024) k_norm_forward_long(NormParams a) {
                     const float v = (float)x[c] - mean - left;
                     sq += v * v;
                 }
-                row_sum2<1024>(sq, none, box, turn);
+                row_sum<1024, 1>(sq, none, box, turn);
                 var = sq / (float)d;
             } else {
                 var -= left * left;

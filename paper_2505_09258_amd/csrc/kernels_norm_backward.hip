@@ -16,62 +16,79 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     __shared__ float sums[G > 1 ? 2 * 256 * NE : 1];
     int turn = 0;
     const int d = a.dim, lane = threadIdx.x % T;
-    const bool quads = (d & 3) == 0;
-    const int64_t groups = (int64_t)gridDim.x * G;
-    float w[NE], dw[NE], db[NE];
-    load_parameter<NE, T>(a.weight, a.weight_type, 1.f, d, lane, quads, w);
-#pragma unroll
-    for (int k = 0; k < NE; ++k) dw[k] = db[k] = 0.f;
-    for (int64_t r0 = ((int64_t)blockIdx.x * G + threadIdx.x / T) * R; r0 < a.rows; r0 += groups * R) {
-        float x[R][NE], g[R][NE], mean[R], rstd[R];
+    const float inv_d = 1.f / (float)d;
+    const int64_t stride = (int64_t)gridDim.x * G * R;
+    RowColumns<XT, S> next_x[R];
+    RowColumns<YT, S> next_g[R];
+    float next_mean[R], next_rstd[R];
+    auto load = [&](int64_t r0) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const XT* src = r0 + i < a.rows ? source_row<XT>(a, r0 + i, lane == 0) : nullptr;
-            mean[i] = rstd[i] = 0.f;
+            next_mean[i] = next_rstd[i] = 0.f;
             if (src) {
-                load_columns<NE, T>(src, d, lane, quads, x[i]);
-                load_columns<NE, T>(static_cast<const YT*>(a.dy) + (r0 + i) * a.dy_stride, d, lane, quads, g[i]);
-                mean[i] = a.mean[r0 + i];
-                rstd[i] = a.rstd[r0 + i];
-            } else {
-#pragma unroll
-                for (int k = 0; k < NE; ++k) x[i][k] = g[i][k] = 0.f;      // nothing to add, a gradient of zeros
+                next_x[i].load(src, d, lane);
+                next_g[i].load(static_cast<const YT*>(a.dy) + (r0 + i) * a.dy_stride, d, lane);
+                next_mean[i] = a.mean[r0 + i];
+                next_rstd[i] = a.rstd[r0 + i];
+            } else {                             // nothing to add, a gradient of zeros
+                next_x[i].clear();
+                next_g[i].clear();
             }
         }
+    };
+    int64_t r0 = ((int64_t)blockIdx.x * G + threadIdx.x / T) * R;
+    load(r0);
+    float w[NE], dw[NE], db[NE];
+    load_parameter<S>(a.weight, a.weight_type, 1.f, d, lane, w);
+#pragma unroll
+    for (int k = 0; k < NE; ++k) dw[k] = db[k] = 0.f;
+    for (; r0 < a.rows; r0 += stride) {
+        float x[R][NE], g[R][NE], rstd[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            rstd[i] = next_rstd[i];
+#pragma unroll
+            for (int k = 0; k < NE; ++k) {
+                // (an access behind the row's end holds the row's last columns: what their zero gradients meet is of no account)
+                x[i][k] = (next_x[i].number(k) - next_mean[i]) * rstd[i];
+                g[i][k] = S::inside(k, lane, d) ? next_g[i].number(k) : 0.f;
+            }
+        }
+        if (r0 + stride < a.rows) load(r0 + stride);          // the next rows arrive while these are worked on
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             if (r0 + i >= a.rows) continue;
             float su = 0.f, sx = 0.f;
 #pragma unroll
             for (int k = 0; k < NE; ++k) {
-                x[i][k] = column_of<NE, T>(k, lane, quads) < d ? (x[i][k] - mean[i]) * rstd[i] : 0.f;
-                dw[k] += g[i][k] * x[i][k];
+                dw[k] = fmaf(g[i][k], x[i][k], dw[k]);
                 db[k] += g[i][k];
                 g[i][k] *= w[k];
                 su += g[i][k];
-                sx += g[i][k] * x[i][k];
+                sx = fmaf(g[i][k], x[i][k], sx);
             }
             if (!a.dx) continue;
-            row_sum2<T>(su, sx, box, turn);
-            su /= (float)d;
-            sx /= (float)d;
+            row_sum<T, 2>(su, sx, box, turn);
+            su *= inv_d;
+            sx *= inv_d;
 #pragma unroll
-            for (int k = 0; k < NE; ++k) g[i][k] = rstd[i] * (g[i][k] - su - x[i][k] * sx);
-            store_columns<NE, T>(static_cast<XT*>(a.dx) + (r0 + i) * a.dx_stride, d, lane, quads, g[i]);
+            for (int k = 0; k < NE; ++k) g[i][k] = rstd[i] * fmaf(-x[i][k], sx, g[i][k] - su);
+            store_columns<S>(static_cast<XT*>(a.dx) + (r0 + i) * a.dx_stride, d, lane, g[i]);
         }
     }
     if (!a.partial) return;
     float* out = a.partial + (int64_t)blockIdx.x * 2 * d;
     if (G == 1) {
-        store_columns<NE, T>(out, d, lane, quads, dw);
-        store_columns<NE, T>(out + d, d, lane, quads, db);
+        store_columns<S>(out, d, lane, dw);
+        store_columns<S>(out + d, d, lane, db);
         return;
     }
     float* mine = sums + (threadIdx.x / T) * (2 * T * NE);
 #pragma unroll
     for (int k = 0; k < NE; ++k) {
-        mine[column_of<NE, T>(k, lane, quads)] = dw[k];
-        mine[T * NE + column_of<NE, T>(k, lane, quads)] = db[k];
+        mine[S::column(k, lane)] = dw[k];
+        mine[T * NE + S::column(k, lane)] = db[k];
     }
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * T * NE; c += S::threads) {
@@ -115,7 +132,7 @@ __global__ void __launch_bounds__(1024) k_norm_backward_long(NormParams a) {
         }
         first = false;
         if (!dx) continue;
-        row_sum2<1024>(su, sx, box, turn);
+        row_sum<1024, 2>(su, sx, box, turn);
         su /= (float)d;
         sx /= (float)d;
         for (int c = threadIdx.x; c < d; c += 1024) {

@@ -53,102 +53,124 @@ __device__ inline float lanes_sum(float v) {
     return v;
 }
 
-// Sums of two numbers over the T threads of a row, in all of them.  Rows of more than a wave have the workgroup to themselves;
-// `box` holds 2 x 16 floats, `turn` alternates so that one barrier a sum is enough.
-template <int T>
-__device__ inline void row_sum2(float& p, float& q, float (*box)[32], int& turn) {
+// Sum of one number, or sums of two, over the T threads of a row, in all of them.  Rows of more than a wave have the workgroup to
+// themselves; `turn` alternates between two boxes, so that one barrier a sum is enough.
+template <int T, int N>
+__device__ inline void row_sum(float& p, float& q, float (*box)[32], int& turn) {
     p = lanes_sum<(T < kWave ? T : kWave)>(p);
-    q = lanes_sum<(T < kWave ? T : kWave)>(q);
+    if (N > 1) q = lanes_sum<(T < kWave ? T : kWave)>(q);
     if (T <= kWave) return;
     constexpr int W = T / kWave;
     float* b = box[turn];
     turn ^= 1;
     if (lane_id() == 0) {
         b[threadIdx.x / kWave] = p;
-        b[16 + threadIdx.x / kWave] = q;
+        if (N > 1) b[16 + threadIdx.x / kWave] = q;
     }
     __syncthreads();
-    p = q = 0.f;
+    p = b[0];
 #pragma unroll
-    for (int k = 0; k < W; ++k) { p += b[k]; q += b[16 + k]; }
+    for (int k = 1; k < W; ++k) p += b[k];
+    if (N < 2) return;
+    q = b[16];
+#pragma unroll
+    for (int k = 1; k < W; ++k) q += b[16 + k];
 }
 
-// The NE columns of a row that thread `lane` of T holds: groups of four (16- or 8-byte accesses) where the dimension is a
-// multiple of four, else single elements, neighbours in neighbouring threads.
-template <int NE, int T>
-__device__ inline int column_of(int k, int lane, bool quads) { return quads ? (k >> 2) * (4 * T) + lane * 4 + (k & 3) : k * T + lane; }
+// How a row is dealt to threads: NE columns a thread, T threads a row, R rows at a time, rows of more than LOW columns.  Q:
+// groups of four columns (16- or 8-byte accesses at any address), for dimensions that are a multiple of four; otherwise single columns,
+// neighbours in neighbouring threads.
+template <int NE_, int T_, int R_, int LOW_, bool Q_>
+struct NormShape {
+    static constexpr int NE = NE_, T = T_, R = R_, LOW = LOW_;
+    static constexpr bool Q = Q_;
+    static constexpr int threads = T_ < 256 ? 256 : T_;      // of a workgroup
+    static constexpr int groups = threads / T_;              // rows that a workgroup holds at a time, R times over
+    static __device__ int column(int k, int lane) { return Q ? (k >> 2) * (4 * T) + lane * 4 + (k & 3) : k * T + lane; }
+    // first column of the access that column k belongs to, and whether it lies in the row (always, below LOW)
+    static __device__ int access(int k, int lane) { return Q ? (k >> 2) * (4 * T) + lane * 4 : k * T + lane; }
+    static __device__ bool inside(int k, int lane, int dim) {
+        return (Q ? ((k >> 2) + 1) * (4 * T) : (k + 1) * T) <= LOW || access(k, lane) < dim;
+    }
+};
+constexpr int kNormRowMax = 16384;           // longer rows do not fit a workgroup's registers
 
-template <int NE, int T, class E>
-__device__ inline void load_columns(const E* row, int dim, int lane, bool quads, float* out) {
-    if (quads) {
+template <bool Q, class F>
+auto for_columns(int dim, F&& f) {
+    if (dim <= 32) return f(NormShape<4, 8, 4, 0, Q>{});
+    if (dim <= 64) return f(NormShape<4, 16, 4, 32, Q>{});
+    if (dim <= 128) return f(NormShape<4, 32, 4, 64, Q>{});
+    if (dim <= 256) return f(NormShape<4, 64, 4, 128, Q>{});
+    if (dim <= 512) return f(NormShape<8, 64, 2, 256, Q>{});
+    if (dim <= 1024) return f(NormShape<16, 64, 1, 512, Q>{});
+    if (dim <= 2048) return f(NormShape<8, 256, 1, 1024, Q>{});
+    if (dim <= 4096) return f(NormShape<16, 256, 1, 2048, Q>{});
+    if (dim <= 8192) return f(NormShape<8, 1024, 1, 4096, Q>{});
+    return f(NormShape<16, 1024, 1, 8192, Q>{});
+}
+template <class F>
+auto for_shape(int dim, F&& f) { return dim % 4 == 0 ? for_columns<true>(dim, f) : for_columns<false>(dim, f); }
+
+// A thread's columns of a row as they lie in memory.  Accesses behind the row's end read its last columns instead: no branch
+// between the loads; `inside` says which numbers count.
+template <class E, class S>
+struct RowColumns {
+    typedef E quad __attribute__((ext_vector_type(4)));
+    quad v[S::NE / 4];
+    __device__ void load(const E* row, int dim, int lane) {
+        if (S::Q) {
 #pragma unroll
-        for (int k = 0; k < NE; k += 4) {
-            const int c = column_of<NE, T>(k, lane, true);
-            if (c < dim) load_quad(row + c, out + k);
-            else out[k] = out[k + 1] = out[k + 2] = out[k + 3] = 0.f;
-        }
-    } else {
+            for (int k = 0; k < S::NE; k += 4) {
+                const int c = S::access(k, lane);
+                v[k / 4] = *reinterpret_cast<const typename Quad<E>::type*>(row + (S::inside(k, lane, dim) ? c : dim - 4));
+            }
+        } else {
 #pragma unroll
-        for (int k = 0; k < NE; ++k) {
-            const int c = column_of<NE, T>(k, lane, false);
-            out[k] = c < dim ? (float)row[c] : 0.f;
+            for (int k = 0; k < S::NE; ++k) {
+                const int c = S::access(k, lane);
+                v[k / 4][k % 4] = row[S::inside(k, lane, dim) ? c : dim - 1];
+            }
         }
     }
-}
-
-template <int NE, int T, class E>
-__device__ inline void store_columns(E* row, int dim, int lane, bool quads, const float* in) {
-    if (quads) {
+    __device__ void clear() {
 #pragma unroll
-        for (int k = 0; k < NE; k += 4) {
-            const int c = column_of<NE, T>(k, lane, true);
-            if (c < dim) store_quad(row + c, in + k);
-        }
+        for (int k = 0; k < S::NE / 4; ++k) v[k] = (quad)(E)0.f;
+    }
+    __device__ float number(int k) const { return (float)v[k / 4][k % 4]; }
+};
+
+template <class S, class E>
+__device__ inline void store_columns(E* row, int dim, int lane, const float* in) {
+    if (S::Q) {
+#pragma unroll
+        for (int k = 0; k < S::NE; k += 4)
+            if (S::inside(k, lane, dim)) store_quad(row + S::access(k, lane), in + k);
     } else {
 #pragma unroll
-        for (int k = 0; k < NE; ++k) {
-            const int c = column_of<NE, T>(k, lane, false);
-            if (c < dim) row[c] = (E)in[k];
-        }
+        for (int k = 0; k < S::NE; ++k)
+            if (S::inside(k, lane, dim)) row[S::access(k, lane)] = (E)in[k];
     }
 }
 
 // weight or bias as fp32, `none` where there is none
-template <int NE, int T>
-__device__ inline void load_parameter(const void* p, int type, float none, int dim, int lane, bool quads, float* out) {
+template <class S>
+__device__ inline void load_parameter(const void* p, int type, float none, int dim, int lane, float* out) {
+    auto take = [&](auto e) {
+        RowColumns<decltype(e), S> r;
+        r.load(static_cast<const decltype(e)*>(p), dim, lane);
+#pragma unroll
+        for (int k = 0; k < S::NE; ++k) out[k] = r.number(k);
+    };
     if (!p) {
 #pragma unroll
-        for (int k = 0; k < NE; ++k) out[k] = none;
+        for (int k = 0; k < S::NE; ++k) out[k] = none;
     } else if (type == LEGEND_TYPE_FLOAT) {
-        load_columns<NE, T>(static_cast<const float*>(p), dim, lane, quads, out);
+        take(float{});
     } else if (type == LEGEND_TYPE_BFLOAT) {
-        load_columns<NE, T>(static_cast<const bf16_t*>(p), dim, lane, quads, out);
+        take(bf16_t{});
     } else {
-        load_columns<NE, T>(static_cast<const half_t*>(p), dim, lane, quads, out);
+        take(half_t{});
     }
-}
-
-// How a row of `dim` columns is dealt to threads: f(NE, T, R): NE columns a thread, T threads a row, R rows at a time.
-template <int NE_, int T_, int R_>
-struct NormShape {
-    static constexpr int NE = NE_, T = T_, R = R_;
-    static constexpr int threads = T_ < 256 ? 256 : T_;      // of a workgroup
-    static constexpr int groups = threads / T_;              // rows that a workgroup holds at a time, R times over
-};
-constexpr int kNormRowMax = 16384;           // longer rows do not fit a workgroup's registers
-
-template <class F>
-auto for_shape(int dim, F&& f) {
-    if (dim <= 32) return f(NormShape<4, 8, 4>{});
-    if (dim <= 64) return f(NormShape<4, 16, 4>{});
-    if (dim <= 128) return f(NormShape<4, 32, 4>{});
-    if (dim <= 256) return f(NormShape<4, 64, 4>{});
-    if (dim <= 512) return f(NormShape<8, 64, 2>{});
-    if (dim <= 1024) return f(NormShape<16, 64, 1>{});
-    if (dim <= 2048) return f(NormShape<8, 256, 1>{});
-    if (dim <= 4096) return f(NormShape<16, 256, 1>{});
-    if (dim <= 8192) return f(NormShape<8, 1024, 1>{});
-    return f(NormShape<16, 1024, 1>{});
 }
 
 template <class F>
