@@ -424,7 +424,7 @@ int legend_adamw_create(legend_ctx* c, const legend_adamw_config* cfg, const leg
     o->d_grads = reinterpret_cast<const void**>(p); p += b_grads;
     o->d_unit_tensor = reinterpret_cast<int32_t*>(p);
     AdamState s;
-    adam_state_at(&s, 0, cfg->beta1, cfg->beta2, cfg->seed);
+    adam_state_at(&s, 0, cfg->beta1, cfg->beta2);
     DENSE_TRY(c, hipMemcpyAsync(o->d_state, &s, sizeof s, hipMemcpyHostToDevice, v.stream));
     DENSE_TRY(c, hipMemcpyAsync(o->d_tensors, desc.data(), sizeof(AdamTensor) * (size_t)n, hipMemcpyHostToDevice, v.stream));
     DENSE_TRY(c, hipMemcpyAsync(o->d_grads, grads.data(), sizeof(void*) * (size_t)n, hipMemcpyHostToDevice, v.stream));
@@ -540,7 +540,7 @@ int legend_adamw_set_steps(legend_adamw* o, int64_t steps) {
     rc = refuse_recording(o->ctx, v.stream, "steps cannot be set");
     if (rc) return rc;
     AdamState s;
-    adam_state_at(&s, steps, o->cfg.beta1, o->cfg.beta2, o->cfg.seed);
+    adam_state_at(&s, steps, o->cfg.beta1, o->cfg.beta2);
     DENSE_TRY(o->ctx, hipMemcpyAsync(o->d_state, &s, sizeof s, hipMemcpyHostToDevice, v.stream));
     DENSE_TRY(o->ctx, hipStreamSynchronize(v.stream));
     return LEGEND_OK;

@@ -245,11 +245,27 @@ __device__ inline void part_block(const AdamTensor& t, const void* grad, const S
     }
 }
 
+// What a step reads of the state and what it leaves lie apart: its first kernel (this one's first thread, in the kernel of the
+// squares, or alone) makes the one from the other, its last writes the other.  No workgroup waits for another, and a counter of
+// finished workgroups, which would tell the last one, costs 10 ns for each of them.
+__device__ inline void begin_step(const AdamParams& a) {
+    AdamState& st = *a.state;
+    st.inv_bias1 = 1.0 / (1.0 - st.power1);
+    st.inv_bias2_root = (float)(1.0 / sqrt(1.0 - st.power2));
+    st.key = hash_fold(a.seed, (uint64_t)(st.steps + 1));
+    st.now_steps = st.steps;
+    st.now_skipped = st.skipped;
+    st.now_power1 = st.power1;
+    st.now_power2 = st.power2;
+}
+__global__ void k_begin_step(AdamParams a) { begin_step(a); }
+
 // K: blocks that a wave takes of a unit (unit_elems = 4 K blocks).
 template <int K>
 __global__ void __launch_bounds__(256) k_grad_squares(AdamParams a) {
     __shared__ double box[4];
     double s[4] = {0.0, 0.0, 0.0, 0.0};
+    if (blockIdx.x == 0 && threadIdx.x == 0) begin_step(a);
     const TensorTable tensors = (TensorTable)a.tensors;
     const UnitTable units = (UnitTable)a.unit_tensor;
     const GradTable grads = (GradTable)a.grads;
@@ -283,7 +299,6 @@ __global__ void __launch_bounds__(256) k_grad_squares(AdamParams a) {
 template <int K>
 __global__ void __launch_bounds__(256) k_adamw(AdamParams a, int norm_parts) {
     __shared__ double box[4];
-    // the state before this step; the last workgroup to be done writes the next one over it
     const double inv_bias1 = a.state->inv_bias1;
     const uint64_t key = a.state->key;
     Step s;
@@ -332,44 +347,32 @@ __global__ void __launch_bounds__(256) k_adamw(AdamParams a, int norm_parts) {
         }
     }
 
-    // Every workgroup has read the state before it counts itself; no memory needs to be ordered for the last one.
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const uint32_t done = __hip_atomic_fetch_add(&a.state->ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (done + 1 == gridDim.x) {
-            a.state->ticket = 0;
-            if (skip) {
-                a.state->skipped += 1;
-            } else {
-                const int64_t steps = a.state->steps + 1;
-                a.state->steps = steps;
-                a.state->inv_bias1 = 1.0 / (1.0 - pow(a.beta1, (double)(steps + 1)));
-                a.state->inv_bias2_root = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)(steps + 1))));
-                a.state->key = hash_fold(a.seed, (uint64_t)(steps + 1));
-            }
-        }
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        AdamState& st = *a.state;
+        st.steps = st.now_steps + (skip ? 0 : 1);
+        st.skipped = st.now_skipped + (skip ? 1 : 0);
+        st.power1 = st.now_power1 * (skip ? 1.0 : a.beta1);
+        st.power2 = st.now_power2 * (skip ? 1.0 : a.beta2);
     }
 }
 
 // Small sets: units of 1024, so that more workgroups share them.  Large ones: 4096, so that a wave has four blocks' loads in flight.
 int adam_unit_elems(int64_t total) { return total >= kLargeTotal ? 4096 : 1024; }
 
-void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2, uint64_t seed) {
+void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2) {
     *s = AdamState{};
     s->steps = steps;
-    s->inv_bias1 = 1.0 / (1.0 - std::pow(beta1, (double)(steps + 1)));
-    s->inv_bias2_root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)(steps + 1))));
-    s->key = hash_fold(seed, (uint64_t)(steps + 1));
+    s->power1 = std::pow(beta1, (double)(steps + 1));
+    s->power2 = std::pow(beta2, (double)(steps + 1));
 }
 
 template <int K>
 static hipError_t launch_units(hipStream_t st, const AdamParams& a) {
     const int parts = (int)(a.units < kAdamNormParts ? a.units : kAdamNormParts);
-    if (a.with_norm && parts > 0) {
-        k_grad_squares<K><<<parts, 256, 0, st>>>(a);
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
+    if (a.with_norm && parts > 0) k_grad_squares<K><<<parts, 256, 0, st>>>(a);
+    else k_begin_step<<<1, 1, 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     const int64_t grid = a.units < 1 ? 1 : (a.units < kStepGrid ? a.units : kStepGrid);
     k_adamw<K><<<(unsigned)grid, 256, 0, st>>>(a, parts);
     return hipGetLastError();

@@ -89,52 +89,78 @@ __global__ void __launch_bounds__(S::threads) k_norm_forward(NormParams a) {
     }
 }
 
-// ---- rows of any length: a workgroup a row, which it reads again for every sweep --------------------------------------
+// ---- rows that do not fit a workgroup's registers: 16384 columns at a time, read again for every sweep ----------------
 
-template <class XT, class YT>
+template <class XT, class YT, bool Q>
 __global__ void __launch_bounds__(1024) k_norm_forward_long(NormParams a) {
+    typedef NormShape<16, 1024, 1, 0, Q> S;
+    constexpr int NE = S::NE, PANEL = S::NE * S::T;
     __shared__ float box[2][32];
     int turn = 0;
-    const int d = a.dim;
+    const int d = a.dim, lane = threadIdx.x;
+    const float inv_d = 1.f / (float)d;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const XT* x = source_row<XT>(a, r, threadIdx.x == 0);
+        const XT* x = source_row<XT>(a, r, lane == 0);
         YT* y = static_cast<YT*>(a.y) + r * a.y_stride;
         float mean = 0.f, rstd = 0.f, left = 0.f, none = 0.f;
-        if (x) {
-            for (int c = threadIdx.x; c < d; c += 1024) mean += (float)x[c];
-            row_sum<1024, 1>(mean, none, box, turn);
-            mean /= (float)d;
-            float sq = 0.f;
-            for (int c = threadIdx.x; c < d; c += 1024) {
-                const float v = (float)x[c] - mean;
-                left += v;
-                sq += v * v;
+        float v[NE];
+        // f(first column, columns left): `v` holds the panel's numbers less `shift`, zeros behind the row's end
+        auto sweep = [&](float shift, auto&& f) {
+            for (int at = 0; at < d; at += PANEL) {
+                RowColumns<XT, S> p;
+                p.load(x + at, d - at, lane);
+#pragma unroll
+                for (int k = 0; k < NE; ++k) v[k] = S::inside(k, lane, d - at) ? p.number(k) - shift : 0.f;
+                f(at, d - at);
             }
+        };
+        if (x) {
+            sweep(0.f, [&](int, int) {
+#pragma unroll
+                for (int k = 0; k < NE; ++k) mean += v[k];
+            });
+            row_sum<1024, 1>(mean, none, box, turn);
+            mean *= inv_d;
+            float sq = 0.f;
+            sweep(mean, [&](int, int) {
+#pragma unroll
+                for (int k = 0; k < NE; ++k) {
+                    left += v[k];
+                    sq = fmaf(v[k], v[k], sq);
+                }
+            });
             row_sum<1024, 2>(left, sq, box, turn);
-            left /= (float)d;
-            float var = sq / (float)d;
+            left *= inv_d;
+            float var = sq * inv_d;
             if (left * left > kLeftShare * var) {
                 sq = 0.f;
-                for (int c = threadIdx.x; c < d; c += 1024) {
-                    const float v = (float)x[c] - mean - left;
-                    sq += v * v;
-                }
+                sweep(mean, [&](int, int n) {
+#pragma unroll
+                    for (int k = 0; k < NE; ++k) {
+                        const float c = S::inside(k, lane, n) ? v[k] - left : 0.f;
+                        sq = fmaf(c, c, sq);
+                    }
+                });
                 row_sum<1024, 1>(sq, none, box, turn);
-                var = sq / (float)d;
+                var = sq * inv_d;
             } else {
-                var -= left * left;
+                var = fmaf(-left, left, var);
             }
-            rstd = 1.0f / sqrtf(var + a.eps);
-            for (int c = threadIdx.x; c < d; c += 1024) {
-                float v = ((float)x[c] - mean - left) * rstd;
-                if (a.weight) v *= load_as(a.weight, c, a.weight_type);
-                if (a.bias) v += load_as(a.bias, c, a.weight_type);
-                y[c] = (YT)v;
-            }
+            rstd = 1.f / sqrtf(var + a.eps);
+            sweep(mean, [&](int at, int n) {
+                float w[NE], b[NE];
+                load_parameter<S>(a.weight, a.weight_type, 1.f, n, lane, w, at);
+                load_parameter<S>(a.bias, a.weight_type, 0.f, n, lane, b, at);
+#pragma unroll
+                for (int k = 0; k < NE; ++k) v[k] = fmaf((v[k] - left) * rstd, w[k], b[k]);
+                store_columns<S>(y + at, n, lane, v);
+            });
         } else {
-            for (int c = threadIdx.x; c < d; c += 1024) y[c] = (YT)0.f;
+#pragma unroll
+            for (int k = 0; k < NE; ++k) v[k] = 0.f;
+            for (int at = 0; at < d; at += PANEL) store_columns<S>(y + at, d - at, lane, v);
         }
-        if (threadIdx.x == 0) {
+        if (lane == 0) {
             if (a.mean) a.mean[r] = mean + left;
             if (a.rstd) a.rstd[r] = rstd;
         }
@@ -146,9 +172,10 @@ hipError_t launch_norm_forward(hipStream_t st, const NormParams& a) {
     return for_types(a.x_type, a.y_type, [&](auto xt, auto yt) {
         if (a.dim > kNormRowMax) {
             const unsigned grid = (unsigned)(a.rows < 512 ? a.rows : 512);
-            k_norm_forward_long<decltype(xt), decltype(yt)><<<grid, 1024, 0, st>>>(a);
+            if (a.dim % 4 == 0) k_norm_forward_long<decltype(xt), decltype(yt), true><<<grid, 1024, 0, st>>>(a);
+            else k_norm_forward_long<decltype(xt), decltype(yt), false><<<grid, 1024, 0, st>>>(a);
         } else {
-            for_shape(a.dim, [&](auto s) {
+            for_shape<1>(a.dim, [&](auto s) {
                 typedef decltype(s) S;
                 // at most the 2048 threads that a compute unit holds, so that weight and bias are loaded once a workgroup
                 const int64_t need = (a.rows + S::groups * S::R - 1) / (S::groups * S::R), most = 256 * 2048 / S::threads;

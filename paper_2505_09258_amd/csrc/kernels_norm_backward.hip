@@ -12,6 +12,7 @@ namespace legend {
 template <class XT, class YT, class S>
 __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     constexpr int NE = S::NE, T = S::T, R = S::R, G = S::groups;
+    constexpr bool KEEP = NE < 32;               // the weight in registers; longer rows read it again for every row (from L2)
     __shared__ float box[2][32];
     __shared__ float sums[G > 1 ? 2 * 256 * NE : 1];
     int turn = 0;
@@ -40,7 +41,7 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     int64_t r0 = ((int64_t)blockIdx.x * G + threadIdx.x / T) * R;
     load(r0);
     float w[NE], dw[NE], db[NE];
-    load_parameter<S>(a.weight, a.weight_type, 1.f, d, lane, w);
+    if (KEEP) load_parameter<S>(a.weight, a.weight_type, 1.f, d, lane, w);
 #pragma unroll
     for (int k = 0; k < NE; ++k) dw[k] = db[k] = 0.f;
     for (; r0 < a.rows; r0 += stride) {
@@ -55,6 +56,7 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
                 g[i][k] = S::inside(k, lane, d) ? next_g[i].number(k) : 0.f;
             }
         }
+        if (!KEEP) load_parameter<S>(a.weight, a.weight_type, 1.f, d, lane, w);
         if (r0 + stride < a.rows) load(r0 + stride);          // the next rows arrive while these are worked on
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -100,49 +102,88 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     }
 }
 
-// ---- rows of any length ------------------------------------------------------------------------------------------------
+// ---- rows that do not fit a workgroup's registers: 16384 columns at a time ---------------------------------------------
 
-template <class XT, class YT>
+template <class XT, class YT, bool Q>
 __global__ void __launch_bounds__(1024) k_norm_backward_long(NormParams a) {
+    typedef NormShape<16, 1024, 1, 0, Q> S;
+    constexpr int NE = S::NE, PANEL = S::NE * S::T;
     __shared__ float box[2][32];
     int turn = 0;
-    const int d = a.dim;
+    const int d = a.dim, lane = threadIdx.x;
+    const float inv_d = 1.f / (float)d;
     float* pw = a.partial + (int64_t)blockIdx.x * 2 * d;       // sums of this workgroup's rows
     float* pb = pw + d;
     bool first = true;
+    float xh[NE], g[NE], w[NE];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const XT* x = source_row<XT>(a, r, threadIdx.x == 0);
+        const XT* x = source_row<XT>(a, r, lane == 0);
         const YT* dy = static_cast<const YT*>(a.dy) + r * a.dy_stride;
         XT* dx = a.dx ? static_cast<XT*>(a.dx) + r * a.dx_stride : nullptr;
         if (!x) {
-            if (dx) for (int c = threadIdx.x; c < d; c += 1024) dx[c] = (XT)0.f;
+#pragma unroll
+            for (int k = 0; k < NE; ++k) g[k] = 0.f;
+            if (dx) for (int at = 0; at < d; at += PANEL) store_columns<S>(dx + at, d - at, lane, g);
             continue;
         }
         const float mean = a.mean[r], rstd = a.rstd[r];
-        float su = 0.f, sx = 0.f;
-        for (int c = threadIdx.x; c < d; c += 1024) {
-            const float g = (float)dy[c], xh = ((float)x[c] - mean) * rstd;
-            const float u = a.weight ? g * load_as(a.weight, c, a.weight_type) : g;
-            su += u;
-            sx += u * xh;
-            if (a.partial) {
-                pw[c] = first ? g * xh : pw[c] + g * xh;
-                pb[c] = first ? g : pb[c] + g;
+        auto take = [&](int at) {
+            RowColumns<XT, S> px;
+            RowColumns<YT, S> pg;
+            px.load(x + at, d - at, lane);
+            pg.load(dy + at, d - at, lane);
+            load_parameter<S>(a.weight, a.weight_type, 1.f, d - at, lane, w, at);
+#pragma unroll
+            for (int k = 0; k < NE; ++k) {
+                xh[k] = (px.number(k) - mean) * rstd;
+                g[k] = S::inside(k, lane, d - at) ? pg.number(k) : 0.f;
             }
+        };
+        float su = 0.f, sx = 0.f;
+        for (int at = 0; at < d; at += PANEL) {
+            take(at);
+#pragma unroll
+            for (int k = 0; k < NE; ++k) {
+                const float u = g[k] * w[k];
+                su += u;
+                sx = fmaf(u, xh[k], sx);
+            }
+            if (!a.partial) continue;
+            RowColumns<float, S> pw_old, pb_old;
+            if (first) {
+                pw_old.clear();
+                pb_old.clear();
+            } else {
+                pw_old.load(pw + at, d - at, lane);
+                pb_old.load(pb + at, d - at, lane);
+            }
+#pragma unroll
+            for (int k = 0; k < NE; ++k) {
+                xh[k] = fmaf(g[k], xh[k], pw_old.number(k));
+                g[k] += pb_old.number(k);
+            }
+            store_columns<S>(pw + at, d - at, lane, xh);
+            store_columns<S>(pb + at, d - at, lane, g);
         }
         first = false;
         if (!dx) continue;
         row_sum<1024, 2>(su, sx, box, turn);
-        su /= (float)d;
-        sx /= (float)d;
-        for (int c = threadIdx.x; c < d; c += 1024) {
-            const float g = (float)dy[c], xh = ((float)x[c] - mean) * rstd;
-            const float u = a.weight ? g * load_as(a.weight, c, a.weight_type) : g;
-            dx[c] = (XT)(rstd * (u - su - xh * sx));
+        su *= inv_d;
+        sx *= inv_d;
+        for (int at = 0; at < d; at += PANEL) {
+            take(at);
+#pragma unroll
+            for (int k = 0; k < NE; ++k) g[k] = rstd * fmaf(-xh[k], sx, g[k] * w[k] - su);
+            store_columns<S>(dx + at, d - at, lane, g);
         }
     }
-    if (a.partial && first)
-        for (int c = threadIdx.x; c < d; c += 1024) pw[c] = pb[c] = 0.f;
+    if (!a.partial || !first) return;
+#pragma unroll
+    for (int k = 0; k < NE; ++k) g[k] = 0.f;
+    for (int at = 0; at < d; at += PANEL) {
+        store_columns<S>(pw + at, d - at, lane, g);
+        store_columns<S>(pb + at, d - at, lane, g);
+    }
 }
 
 // Sums of the workgroups' partial sums, in 64 bits: 32 columns a workgroup, each by 32 threads that take every 32nd part, added
@@ -169,13 +210,15 @@ __global__ void __launch_bounds__(1024) k_norm_sums(NormParams a) {
 }
 
 // Workgroups of the backward pass.  With sums wanted, each writes 8 bytes a column, which the second kernel reads again: two a
-// compute unit are enough to keep loads in flight, and few enough that their sums stay a small share of what the rows take.
+// compute unit (one of the long rows' large workgroups) keep enough loads in flight, and their sums stay a small share of what the
+// rows take.
 int norm_parts(int64_t rows, int32_t dim) {
-    int64_t need = rows, most = 512;
+    int64_t need = rows, most = 256;
     if (dim <= kNormRowMax)
-        for_shape(dim, [&](auto s) {
+        for_shape<2>(dim, [&](auto s) {
             typedef decltype(s) S;
             need = (rows + S::groups * S::R - 1) / (S::groups * S::R);
+            if (S::threads <= 256) most = 512;
             return 0;
         });
     return (int)(need < most ? need : most);
@@ -185,9 +228,10 @@ hipError_t launch_norm_backward(hipStream_t st, const NormParams& a) {
     if (a.rows > 0) {
         hipError_t e = for_types(a.x_type, a.dy_type, [&](auto xt, auto yt) {
             if (a.dim > kNormRowMax) {
-                k_norm_backward_long<decltype(xt), decltype(yt)><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
+                if (a.dim % 4 == 0) k_norm_backward_long<decltype(xt), decltype(yt), true><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
+                else k_norm_backward_long<decltype(xt), decltype(yt), false><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
             } else {
-                for_shape(a.dim, [&](auto s) {
+                for_shape<2>(a.dim, [&](auto s) {
                     typedef decltype(s) S;
                     const int64_t need = (a.rows + S::groups * S::R - 1) / (S::groups * S::R), most = 256 * 2048 / S::threads;
                     const unsigned grid = a.partial ? (unsigned)a.parts : (unsigned)(need < most ? need : most);

@@ -236,11 +236,15 @@ struct AdamTensor {
     int32_t param_type, grad_type, state_type, index;
 };
 struct AdamState {                          // device; what the next step needs besides the tensors
+    // written by the step's last kernel
     int64_t steps, skipped;
-    double inv_bias1;                       // 1 / (1 - beta1^t), t = steps + 1
+    double power1, power2;                  // beta1^t, beta2^t, t = steps + 1
+    // written by its first kernel from the above, read by its last
+    double inv_bias1;                       // 1 / (1 - beta1^t)
     float inv_bias2_root;                   // 1 / sqrt(1 - beta2^t)
-    uint32_t ticket;                        // workgroups of the running step that are done
     uint64_t key;                           // fold(seed, t)
+    int64_t now_steps, now_skipped;
+    double now_power1, now_power2;
 };
 struct AdamParams {
     const AdamTensor* tensors;
@@ -256,7 +260,7 @@ struct AdamParams {
     int32_t with_norm;
 };
 int adam_unit_elems(int64_t total);
-void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2, uint64_t seed);
+void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2);
 hipError_t launch_adamw(hipStream_t st, const AdamParams& a);
 
 int64_t update_long_rows_capacity(int64_t n_occ);

@@ -95,21 +95,22 @@ struct NormShape {
 };
 constexpr int kNormRowMax = 16384;           // longer rows do not fit a workgroup's registers
 
-template <bool Q, class F>
+// R: rows of at most 512 columns that a thread group takes at a time
+template <int R, bool Q, class F>
 auto for_columns(int dim, F&& f) {
-    if (dim <= 32) return f(NormShape<4, 8, 4, 0, Q>{});
-    if (dim <= 64) return f(NormShape<4, 16, 4, 32, Q>{});
-    if (dim <= 128) return f(NormShape<4, 32, 4, 64, Q>{});
-    if (dim <= 256) return f(NormShape<4, 64, 4, 128, Q>{});
-    if (dim <= 512) return f(NormShape<8, 64, 2, 256, Q>{});
+    if (dim <= 32) return f(NormShape<4, 8, R, 0, Q>{});
+    if (dim <= 64) return f(NormShape<4, 16, R, 32, Q>{});
+    if (dim <= 128) return f(NormShape<4, 32, R, 64, Q>{});
+    if (dim <= 256) return f(NormShape<4, 64, R, 128, Q>{});
+    if (dim <= 512) return f(NormShape<8, 64, R, 256, Q>{});
     if (dim <= 1024) return f(NormShape<16, 64, 1, 512, Q>{});
     if (dim <= 2048) return f(NormShape<8, 256, 1, 1024, Q>{});
     if (dim <= 4096) return f(NormShape<16, 256, 1, 2048, Q>{});
-    if (dim <= 8192) return f(NormShape<8, 1024, 1, 4096, Q>{});
-    return f(NormShape<16, 1024, 1, 8192, Q>{});
+    if (dim <= 8192) return f(NormShape<16, 512, 1, 4096, Q>{});
+    return f(NormShape<32, 512, 1, 8192, Q>{});
 }
-template <class F>
-auto for_shape(int dim, F&& f) { return dim % 4 == 0 ? for_columns<true>(dim, f) : for_columns<false>(dim, f); }
+template <int R, class F>
+auto for_shape(int dim, F&& f) { return dim % 4 == 0 ? for_columns<R, true>(dim, f) : for_columns<R, false>(dim, f); }
 
 // A thread's columns of a row as they lie in memory.  Accesses behind the row's end read its last columns instead: no branch
 // between the loads; `inside` says which numbers count.
@@ -152,12 +153,12 @@ __device__ inline void store_columns(E* row, int dim, int lane, const float* in)
     }
 }
 
-// weight or bias as fp32, `none` where there is none
+// weight or bias as fp32, from column `at` on, `none` where there is none
 template <class S>
-__device__ inline void load_parameter(const void* p, int type, float none, int dim, int lane, float* out) {
+__device__ inline void load_parameter(const void* p, int type, float none, int dim, int lane, float* out, int at = 0) {
     auto take = [&](auto e) {
         RowColumns<decltype(e), S> r;
-        r.load(static_cast<const decltype(e)*>(p), dim, lane);
+        r.load(static_cast<const decltype(e)*>(p) + at, dim, lane);
 #pragma unroll
         for (int k = 0; k < S::NE; ++k) out[k] = r.number(k);
     };

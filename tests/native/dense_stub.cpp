@@ -46,7 +46,7 @@ int norm_parts(int64_t rows, int32_t) { return (int)(rows < 512 ? rows : 512); }
 hipError_t launch_norm_forward(hipStream_t, const NormParams&) { ++launches; return hipSuccess; }
 hipError_t launch_norm_backward(hipStream_t, const NormParams&) { ++launches; return hipSuccess; }
 int adam_unit_elems(int64_t) { return 1024; }
-void adam_state_at(AdamState* s, int64_t steps, double, double, uint64_t) { *s = AdamState{}; s->steps = steps; }
+void adam_state_at(AdamState* s, int64_t steps, double, double) { *s = AdamState{}; s->steps = steps; }
 hipError_t launch_adamw(hipStream_t, const AdamParams& a) {
     // every unit belongs to its tensor and every tensor is covered
     int64_t u = 0;
