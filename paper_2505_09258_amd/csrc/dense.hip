@@ -26,6 +26,7 @@ struct legend_adamw {
     double* d_partial = nullptr;
     int64_t units = 0;
     int32_t unit_elems = 0;
+    bool stream = false;
 };
 
 namespace {
@@ -215,6 +216,14 @@ int check_tensor(const legend_adamw_tensor& t, int64_t k) {
     return LEGEND_OK;
 }
 
+// Where parameters, states and gradients of all tensors do not fit the Infinity Cache together, a step marks the first two as
+// streaming, so that the gradients, which the norm has just read, are still there for it.  (60 M fp32 parameters, 1.7 GB: 355 against
+// 401 us; 5 M, 140 MB, where everything stays in the cache from step to step: 44 against 39.)
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;
+int64_t tensor_bytes(const legend_adamw_tensor& t) {
+    return t.count * (type_size(t.param_type) + type_size(t.grad_type) + (t.master ? 4 : 0) + (t.state_type == LEGEND_STATE_BLOCK ? 2 : 8));
+}
+
 int refuse_recording(legend_ctx* c, hipStream_t st, const char* what) {
     bool rec = false;
     int rc = recording(c, st, &rec);
@@ -368,15 +377,16 @@ int legend_adamw_create(legend_ctx* c, const legend_adamw_config* cfg, const leg
     if (cfg->reserved != 0) return fail(LEGEND_E_INVAL, "reserved must be 0");
     if (n < 1 || n > (1 << 24)) return fail(LEGEND_E_INVAL, "n must be in [1, 2^24]");
     if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return fail(LEGEND_E_INVAL, "beta1 and beta2 must be in [0, 1)");
-    if (!(cfg->eps > 0.0) || !std::isfinite(cfg->eps)) return fail(LEGEND_E_INVAL, "eps must be positive and finite");
+    if (!(cfg->eps >= 1e-15) || !(cfg->eps <= 1e15)) return fail(LEGEND_E_INVAL, "eps must be in [1e-15, 1e15]");
     if (!(cfg->max_norm >= 0.0) || !std::isfinite(cfg->max_norm)) return fail(LEGEND_E_INVAL, "max_norm must be finite and not negative");
     std::vector<const void*> grads((size_t)n);
-    int64_t total = 0;
+    int64_t total = 0, total_bytes = 0;
     for (int64_t k = 0; k < n; ++k) {
         rc = check_tensor(tensors[k], k);
         if (rc) return rc;
         grads[(size_t)k] = tensors[k].grad;
         total += tensors[k].count;
+        total_bytes += tensor_bytes(tensors[k]);
         if (total > ((int64_t)1 << 48)) return fail(LEGEND_E_INVAL, "too many elements");
     }
     struct Holder {
@@ -397,6 +407,7 @@ int legend_adamw_create(legend_ctx* c, const legend_adamw_config* cfg, const leg
     if (rc) return rc;
 
     o->unit_elems = adam_unit_elems(total);
+    o->stream = total_bytes > kCacheBytes;
     std::vector<AdamTensor> desc((size_t)n);
     for (int64_t k = 0; k < n; ++k) {
         const legend_adamw_tensor& t = tensors[k];
@@ -484,6 +495,7 @@ int legend_adamw_step(legend_adamw* o, double lr, const float* lr_factor, const 
     a.eps = o->cfg.eps;
     a.max_norm = o->cfg.max_norm;
     a.seed = o->cfg.seed;
+    a.stream = o->stream ? 1 : 0;
     a.with_norm = o->cfg.max_norm > 0.0 || norm ? 1 : 0;
     DENSE_TRY(o->ctx, launch_adamw(v.stream, a));
     return LEGEND_OK;

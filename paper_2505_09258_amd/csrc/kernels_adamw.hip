@@ -17,13 +17,29 @@ constexpr float kTopCode = 448.f;           // largest e4m3 value
 constexpr float kLeastCode = 0.001953125f;  // smallest above zero, 2^-9
 constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100: 1 / scale stays far from infinity
 
-constexpr int64_t kLargeTotal = 4 << 20;    // elements
-constexpr int64_t kStepGrid = 2048;         // workgroups of a step: eight a compute unit
+#ifndef KL
+#define KL 2
+#define LT (4 << 20)
+#define SG 2048
+#define NP 1024
+#endif
+constexpr int64_t kLargeTotal = LT;    // elements
+constexpr int64_t kStepGrid = SG;         // workgroups of a step: eight a compute unit
 
-__device__ inline float wave_max(float v) {
-#pragma unroll
-    for (int k = 1; k < kWave; k <<= 1) v = fmaxf(v, wave_shfl_xor(v, k));
-    return v;
+// Largest of the wave's numbers, none below zero, in all lanes.  Compared as integers, which orders them alike, with infinity and
+// NaN at the top.
+template <int CTRL>
+__device__ inline uint32_t dpp_word(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false); }
+__device__ inline float wave_max(float top) {
+    uint32_t v = __float_as_uint(top);
+    v = max(v, dpp_word<0xB1>(v));           // lane ^ 1
+    v = max(v, dpp_word<0x4E>(v));           // lane ^ 2
+    v = max(v, dpp_word<0x141>(v));          // mirrored within 8
+    v = max(v, dpp_word<0x140>(v));          // mirrored within 16
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((uint32_t)r[0], (uint32_t)r[1]);
+    const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return __uint_as_float(max((uint32_t)h[0], (uint32_t)h[1]));
 }
 
 // sum of 256 threads' doubles, in every thread
@@ -45,12 +61,6 @@ __device__ inline uint32_t random_word(uint32_t w) {
     return w ^ (w >> 16);
 }
 
-// e4m3 code of x in units of its scale; the conversion adds the word's upper 20 bits below the last bit that it keeps
-__device__ inline uint8_t to_code(float x, bool finite, uint32_t word) {
-    x = finite ? fminf(fmaxf(x, -kTopCode), kTopCode) : __builtin_nanf("");
-    return (uint8_t)__builtin_amdgcn_cvt_sr_fp8_f32(x, word, 0, 0);
-}
-
 // What a step has in common for all elements of a tensor.
 struct Step {
     float scale, b1, b2, c1, c2, eps, inv_bias2_root;    // of the gradient; beta and 1 - beta; epsilon
@@ -69,14 +79,17 @@ __device__ inline AdamTensor tensor_at(TensorTable p) {
 }
 
 // Four consecutive elements as they lie in memory, and as numbers.
+template <bool STREAM>
 __device__ inline uint4 raw_quad(const void* p, int64_t i, int type) {
     typedef uint32_t two __attribute__((ext_vector_type(2), aligned(2)));
     typedef uint32_t four __attribute__((ext_vector_type(4), aligned(4)));
     if (type == LEGEND_TYPE_FLOAT) {
-        const four v = *reinterpret_cast<const four*>(static_cast<const float*>(p) + i);
+        const four* q = reinterpret_cast<const four*>(static_cast<const float*>(p) + i);
+        const four v = STREAM ? __builtin_nontemporal_load(q) : *q;
         return make_uint4(v.x, v.y, v.z, v.w);
     }
-    const two v = *reinterpret_cast<const two*>(static_cast<const uint16_t*>(p) + i);
+    const two* q = reinterpret_cast<const two*>(static_cast<const uint16_t*>(p) + i);
+    const two v = STREAM ? __builtin_nontemporal_load(q) : *q;
     return make_uint4(v.x, v.y, 0u, 0u);
 }
 __device__ inline void numbers_of(uint4 r, int type, float* out) {
@@ -91,119 +104,159 @@ __device__ inline void numbers_of(uint4 r, int type, float* out) {
         out[0] = (float)lo.x; out[1] = (float)lo.y; out[2] = (float)hi.x; out[3] = (float)hi.y;
     }
 }
+template <bool STREAM>
 __device__ inline void put_quad(void* p, int64_t i, int type, const float* v) {
-    if (type == LEGEND_TYPE_FLOAT) store_quad(static_cast<float*>(p) + i, v);
-    else if (type == LEGEND_TYPE_BFLOAT) store_quad(static_cast<bf16_t*>(p) + i, v);
-    else store_quad(static_cast<half_t*>(p) + i, v);
+    if (type == LEGEND_TYPE_FLOAT) store_quad<STREAM>(static_cast<float*>(p) + i, v);
+    else if (type == LEGEND_TYPE_BFLOAT) store_quad<STREAM>(static_cast<bf16_t*>(p) + i, v);
+    else store_quad<STREAM>(static_cast<half_t*>(p) + i, v);
+}
+__device__ inline void codes_to_numbers(uint32_t codes, float scale, float* out) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+    out[0] = lo[0] * scale; out[1] = lo[1] * scale; out[2] = hi[0] * scale; out[3] = hi[1] * scale;
 }
 
-// Moments and parameter of one element; the root of the new second moment comes back.
+// Moments and parameter of one element; the root of the new second moment comes back.  Root and reciprocal are the hardware's, each
+// within 1.6 half steps of fp32; a second moment below fp32's normal numbers has the root 0.
 __device__ inline float step_element(const Step& s, float g, float& m, float& v, float& p) {
     g *= s.scale;
-    m = s.b1 * m + s.c1 * g;
-    v = s.b2 * v + (s.c2 * g) * g;
-    const float root = sqrtf(v);
-    p = p * s.keep - s.rate * (m / (root * s.inv_bias2_root + s.eps));
+    m = fmaf(s.b1, m, s.c1 * g);
+    v = fmaf(s.b2, v, (s.c2 * g) * g);
+    const float root = __builtin_amdgcn_sqrtf(v);
+    const float down = m * __builtin_amdgcn_rcpf(fmaf(root, s.inv_bias2_root, s.eps));
+    p = fmaf(p, s.keep, -(s.rate * down));
     return root;
 }
 
-// Scale of a block from its lanes' largest finite magnitudes, and its reciprocal.
-__device__ inline float block_scale(float top, float& inverse) {
-    float s = wave_max(top) / kTopCode;
+// Scale of a block from its lanes' largest magnitudes v[0..3], and how many scales a number is: 2^-21 less than the reciprocal
+// says, so that the largest is never above the largest code.  Infinities and NaN do not count.
+__device__ inline float block_scale(const float* v, float& per_scale) {
+    float top = wave_max(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+    if (!(top < __builtin_inff())) {
+        float t = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t = fabsf(v[j]) < __builtin_inff() ? fmaxf(t, fabsf(v[j])) : t;
+        top = wave_max(t);
+    }
+    float s = top * (1.f / kTopCode);
     s = s > kLeastScale ? s : 0.f;
-    inverse = s > 0.f ? 1.f / s : 0.f;
+    per_scale = s > 0.f ? __builtin_amdgcn_rcpf(s) * (1.f - 4.76837158203125e-7f) : 0.f;
     return s;
 }
-__device__ inline float finite_or_zero(float v) { return v < __builtin_inff() ? v : 0.f; }
-__device__ inline void codes_of(float m, float inv_m, float root, float inv_root, uint32_t word, uint8_t& cm, uint8_t& cr) {
-    cm = to_code(m * inv_m, fabsf(m) < __builtin_inff(), word);
-    const float x = root * inv_root;
-    cr = to_code(x > 0.f ? fmaxf(x, kLeastCode) : x, root < __builtin_inff(), word << 16);
+// The e4m3 codes of four first moments and roots.  The conversion adds a word's upper 20 bits below the last bit that it keeps, and
+// gives the NaN code for an infinity.
+__device__ inline void codes_of(const float* m, float m_per, const float* root, float root_per, const uint32_t* words, uint32_t& cm, uint32_t& cr) {
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x[j] = root[j] * root_per;
+        x[j] = x[j] > 0.f ? fmaxf(x[j], kLeastCode) : x[j];
+    }
+    int a = 0, b = 0;
+    a = __builtin_amdgcn_cvt_sr_fp8_f32(m[0] * m_per, words[0], a, 0);
+    b = __builtin_amdgcn_cvt_sr_fp8_f32(x[0], words[0] << 16, b, 0);
+    a = __builtin_amdgcn_cvt_sr_fp8_f32(m[1] * m_per, words[1], a, 1);
+    b = __builtin_amdgcn_cvt_sr_fp8_f32(x[1], words[1] << 16, b, 1);
+    a = __builtin_amdgcn_cvt_sr_fp8_f32(m[2] * m_per, words[2], a, 2);
+    b = __builtin_amdgcn_cvt_sr_fp8_f32(x[2], words[2] << 16, b, 2);
+    a = __builtin_amdgcn_cvt_sr_fp8_f32(m[3] * m_per, words[3], a, 3);
+    b = __builtin_amdgcn_cvt_sr_fp8_f32(x[3], words[3] << 16, b, 3);
+    cm = (uint32_t)a;
+    cr = (uint32_t)b;
 }
 __device__ inline uint32_t block_key(const Step& s, int64_t lo) { return s.key ^ (uint32_t)(lo >> 32) * 0x9E3779B1u; }   // a block never crosses 2^32
 
-// K whole blocks of 256 elements, `apart` elements from one to the next: every load first, then the arithmetic.
-template <int K, bool BLOCK>
-__device__ inline void whole_blocks(const AdamTensor& t, const void* grad, const Step& s, int64_t lo, int64_t apart) {
-    const int64_t i0 = lo + lane_id() * 4;
-    const int ptype = t.master ? (int)LEGEND_TYPE_FLOAT : t.param_type;
-    const void* from = t.master ? t.master : t.param;
-    uint4 rg[K], rp[K], rm[K], rv[K];
-    uint32_t cm[K], cv[K];
-    float ms[K], vs[K];
+// K whole blocks of 256 elements as a wave loads them, kApart elements from one to the next: four neighbouring elements a lane.
+constexpr int kApart = 4 * kAdamBlock;
+typedef uint32_t code_word __attribute__((aligned(1)));
+template <int K, bool STREAM>
+struct Blocks {
+    uint4 g[K], p[K], m[K], v[K];            // 8-bit states: four codes in m.x and v.x, the block's scales in m.y and v.y
+
+    __device__ void load(const AdamTensor& t, const void* grad, int64_t lo) {
+        const int64_t i0 = lo + lane_id() * 4;
+        const int ptype = t.master ? (int)LEGEND_TYPE_FLOAT : t.param_type;
+        const void* from = t.master ? t.master : t.param;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int64_t i = i0 + k * apart;
-        rg[k] = raw_quad(grad, i, t.grad_type);
-        rp[k] = raw_quad(from, i, ptype);
-        if (BLOCK) {
-            typedef uint32_t word __attribute__((aligned(1)));
-            cm[k] = *reinterpret_cast<const word*>(static_cast<const uint8_t*>(t.m) + i);
-            cv[k] = *reinterpret_cast<const word*>(static_cast<const uint8_t*>(t.v) + i);
-            ms[k] = t.m_scale[(lo + k * apart) / kAdamBlock];
-            vs[k] = t.v_scale[(lo + k * apart) / kAdamBlock];
+        for (int k = 0; k < K; ++k) {
+            g[k] = raw_quad<false>(grad, i0 + k * kApart, t.grad_type);
+            p[k] = raw_quad<STREAM>(from, i0 + k * kApart, ptype);
+        }
+        if (t.state_type == LEGEND_STATE_BLOCK) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const code_word* cm = reinterpret_cast<const code_word*>(static_cast<const uint8_t*>(t.m) + i0 + k * kApart);
+                const code_word* cv = reinterpret_cast<const code_word*>(static_cast<const uint8_t*>(t.v) + i0 + k * kApart);
+                m[k].x = STREAM ? __builtin_nontemporal_load(cm) : *cm;
+                v[k].x = STREAM ? __builtin_nontemporal_load(cv) : *cv;
+                m[k].y = __float_as_uint(t.m_scale[lo / kAdamBlock + k * (kApart / kAdamBlock)]);
+                v[k].y = __float_as_uint(t.v_scale[lo / kAdamBlock + k * (kApart / kAdamBlock)]);
+            }
         } else {
-            rm[k] = raw_quad(t.m, i, LEGEND_TYPE_FLOAT);
-            rv[k] = raw_quad(t.v, i, LEGEND_TYPE_FLOAT);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                m[k] = raw_quad<STREAM>(t.m, i0 + k * kApart, LEGEND_TYPE_FLOAT);
+                v[k] = raw_quad<STREAM>(t.v, i0 + k * kApart, LEGEND_TYPE_FLOAT);
+            }
         }
     }
+
+    template <bool BLOCK>
+    __device__ void finish(const AdamTensor& t, const Step& s, int64_t lo) const {
+        const int ptype = t.master ? (int)LEGEND_TYPE_FLOAT : t.param_type;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int64_t i = i0 + k * apart;
-        float g[4], p[4], m[4], v[4], root[4];
-        numbers_of(rg[k], t.grad_type, g);
-        numbers_of(rp[k], ptype, p);
-        if (BLOCK) {
-            m[0] = __builtin_amdgcn_cvt_f32_fp8(cm[k], 0) * ms[k]; m[1] = __builtin_amdgcn_cvt_f32_fp8(cm[k], 1) * ms[k];
-            m[2] = __builtin_amdgcn_cvt_f32_fp8(cm[k], 2) * ms[k]; m[3] = __builtin_amdgcn_cvt_f32_fp8(cm[k], 3) * ms[k];
-            v[0] = __builtin_amdgcn_cvt_f32_fp8(cv[k], 0) * vs[k]; v[1] = __builtin_amdgcn_cvt_f32_fp8(cv[k], 1) * vs[k];
-            v[2] = __builtin_amdgcn_cvt_f32_fp8(cv[k], 2) * vs[k]; v[3] = __builtin_amdgcn_cvt_f32_fp8(cv[k], 3) * vs[k];
+        for (int k = 0; k < K; ++k) {
+            const int64_t i = lo + lane_id() * 4 + k * kApart;
+            float ge[4], pe[4], me[4], ve[4], root[4];
+            numbers_of(g[k], t.grad_type, ge);
+            numbers_of(p[k], ptype, pe);
+            if (BLOCK) {
+                codes_to_numbers(m[k].x, __uint_as_float(m[k].y), me);
+                codes_to_numbers(v[k].x, __uint_as_float(v[k].y), ve);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] *= v[j];
-        } else {
-            numbers_of(rm[k], LEGEND_TYPE_FLOAT, m);
-            numbers_of(rv[k], LEGEND_TYPE_FLOAT, v);
-        }
+                for (int j = 0; j < 4; ++j) ve[j] *= ve[j];
+            } else {
+                numbers_of(m[k], LEGEND_TYPE_FLOAT, me);
+                numbers_of(v[k], LEGEND_TYPE_FLOAT, ve);
+            }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) root[j] = step_element(s, g[j], m[j], v[j], p[j]);
-        if (t.master) store_quad(t.master + i, p);
-        put_quad(t.param, i, t.param_type, p);
-        if (!BLOCK) {
-            store_quad(static_cast<float*>(t.m) + i, m);
-            store_quad(static_cast<float*>(t.v) + i, v);
-            continue;
-        }
-        float top_m = 0.f, top_root = 0.f, inv_m, inv_root;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            top_m = fmaxf(top_m, finite_or_zero(fabsf(m[j])));
-            top_root = fmaxf(top_root, finite_or_zero(root[j]));
-        }
-        const float new_ms = block_scale(top_m, inv_m), new_vs = block_scale(top_root, inv_root);
-        const uint32_t key = block_key(s, lo + k * apart);
-        uint32_t wm = 0, wr = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint8_t a, b;
-            codes_of(m[j], inv_m, root[j], inv_root, random_word((uint32_t)(i + j) ^ key), a, b);
-            wm |= (uint32_t)a << (8 * j);
-            wr |= (uint32_t)b << (8 * j);
-        }
-        typedef uint32_t word __attribute__((aligned(1)));
-        *reinterpret_cast<word*>(static_cast<uint8_t*>(t.m) + i) = wm;
-        *reinterpret_cast<word*>(static_cast<uint8_t*>(t.v) + i) = wr;
-        if (lane_id() == 0) {
-            t.m_scale[(lo + k * apart) / kAdamBlock] = new_ms;
-            t.v_scale[(lo + k * apart) / kAdamBlock] = new_vs;
+            for (int j = 0; j < 4; ++j) root[j] = step_element(s, ge[j], me[j], ve[j], pe[j]);
+            if (t.master) store_quad<STREAM>(t.master + i, pe);
+            put_quad<STREAM>(t.param, i, t.param_type, pe);
+            if (!BLOCK) {
+                store_quad<STREAM>(static_cast<float*>(t.m) + i, me);
+                store_quad<STREAM>(static_cast<float*>(t.v) + i, ve);
+                continue;
+            }
+            const int64_t at = lo + k * kApart;
+            float m_per, root_per;
+            const float ms = block_scale(me, m_per), vs = block_scale(root, root_per);
+            const uint32_t key = block_key(s, at);
+            const uint32_t words[4] = {random_word((uint32_t)i ^ key), random_word((uint32_t)(i + 1) ^ key),
+                                       random_word((uint32_t)(i + 2) ^ key), random_word((uint32_t)(i + 3) ^ key)};
+            uint32_t cm, cr;
+            codes_of(me, m_per, root, root_per, words, cm, cr);
+            code_word* to_m = reinterpret_cast<code_word*>(static_cast<uint8_t*>(t.m) + i);
+            code_word* to_v = reinterpret_cast<code_word*>(static_cast<uint8_t*>(t.v) + i);
+            if (STREAM) {
+                __builtin_nontemporal_store(cm, to_m);
+                __builtin_nontemporal_store(cr, to_v);
+            } else {
+                *to_m = cm;
+                *to_v = cr;
+            }
+            if (lane_id() == 0) {
+                t.m_scale[at / kAdamBlock] = ms;
+                t.v_scale[at / kAdamBlock] = vs;
+            }
         }
     }
-}
+};
 
 // The last block of a tensor, elements [lo, count): single elements, neighbours in neighbouring lanes.
 __device__ inline void part_block(const AdamTensor& t, const void* grad, const Step& s, int64_t lo) {
     const bool block = t.state_type == LEGEND_STATE_BLOCK;
     const float ms = block ? t.m_scale[lo / kAdamBlock] : 1.f, vs = block ? t.v_scale[lo / kAdamBlock] : 1.f;
-    float m[4], root[4], top_m = 0.f, top_root = 0.f;
+    float m[4], root[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t i = lo + j * kWave + lane_id();
@@ -226,18 +279,21 @@ __device__ inline void part_block(const AdamTensor& t, const void* grad, const S
             static_cast<float*>(t.m)[i] = m[j];
             static_cast<float*>(t.v)[i] = v;
         }
-        top_m = fmaxf(top_m, finite_or_zero(fabsf(m[j])));
-        top_root = fmaxf(top_root, finite_or_zero(root[j]));
     }
     if (!block) return;
-    float inv_m, inv_root;
-    const float new_ms = block_scale(top_m, inv_m), new_vs = block_scale(top_root, inv_root);
+    float m_per, root_per;
+    const float new_ms = block_scale(m, m_per), new_vs = block_scale(root, root_per);
     const uint32_t key = block_key(s, lo);
+    uint32_t words[4], cm, cr;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) words[j] = random_word((uint32_t)(lo + j * kWave + lane_id()) ^ key);
+    codes_of(m, m_per, root, root_per, words, cm, cr);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t i = lo + j * kWave + lane_id();
-        if (i < t.count)
-            codes_of(m[j], inv_m, root[j], inv_root, random_word((uint32_t)i ^ key), static_cast<uint8_t*>(t.m)[i], static_cast<uint8_t*>(t.v)[i]);
+        if (i >= t.count) continue;
+        static_cast<uint8_t*>(t.m)[i] = (uint8_t)(cm >> (8 * j));
+        static_cast<uint8_t*>(t.v)[i] = (uint8_t)(cr >> (8 * j));
     }
     if (lane_id() == 0) {
         t.m_scale[lo / kAdamBlock] = new_ms;
@@ -277,7 +333,7 @@ __global__ void __launch_bounds__(256) k_grad_squares(AdamParams a) {
         if (lo + K * 1024 <= count) {
             uint4 r[K];
 #pragma unroll
-            for (int k = 0; k < K; ++k) r[k] = raw_quad(grad, lo + k * 1024 + threadIdx.x * 4, type);
+            for (int k = 0; k < K; ++k) r[k] = raw_quad<false>(grad, lo + k * kApart + threadIdx.x * 4, type);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 float g[4];
@@ -296,56 +352,70 @@ __global__ void __launch_bounds__(256) k_grad_squares(AdamParams a) {
     if (threadIdx.x == 0) a.partial[blockIdx.x] = all;
 }
 
-template <int K>
+template <int K, bool STREAM>
 __global__ void __launch_bounds__(256) k_adamw(AdamParams a, int norm_parts) {
     __shared__ double box[4];
-    const double inv_bias1 = a.state->inv_bias1;
-    const uint64_t key = a.state->key;
-    Step s;
-    s.inv_bias2_root = a.state->inv_bias2_root;
-    s.scale = a.grad_scale ? *a.grad_scale : 1.f;
-    bool skip = false;
-    if (a.with_norm) {
-        double sum = 0.0;
-        for (int k = threadIdx.x; k < norm_parts; k += 256) sum += a.partial[k];
-        const double norm = sqrt(block_sum(sum, box)) * fabs((double)s.scale);
-        skip = !(norm < __builtin_inf());
-        if (a.norm_out && blockIdx.x == 0 && threadIdx.x == 0) *a.norm_out = (float)norm;
-        if (a.max_norm > 0.0 && norm > a.max_norm) s.scale = (float)(a.max_norm / (norm + 1e-6)) * s.scale;
-    }
-    const double lr = a.lr * (a.lr_factor ? (double)*a.lr_factor : 1.0);
-    s.b1 = (float)a.beta1;
-    s.b2 = (float)a.beta2;
-    s.c1 = (float)(1.0 - a.beta1);
-    s.c2 = (float)(1.0 - a.beta2);
-    s.eps = (float)a.eps;
-    const int wave = threadIdx.x / kWave;
     const TensorTable tensors = (TensorTable)a.tensors;
     const UnitTable units = (UnitTable)a.unit_tensor;
     const GradTable grads = (GradTable)a.grads;
-
-    for (int64_t u = skip ? a.units : blockIdx.x; u < a.units; u += gridDim.x) {
+    double lr = 0.0, inv_bias1 = 0.0;
+    uint64_t key = 0;
+    Step s;
+    bool ready = false, skip = false;
+    auto prepare = [&]() {
+        ready = true;
+        inv_bias1 = a.state->inv_bias1;
+        key = a.state->key;
+        s.inv_bias2_root = a.state->inv_bias2_root;
+        s.scale = a.grad_scale ? *a.grad_scale : 1.f;
+        if (a.with_norm) {
+            double sum = 0.0;
+            for (int k = threadIdx.x; k < norm_parts; k += 256) sum += a.partial[k];
+            const double norm = sqrt(block_sum(sum, box)) * fabs((double)s.scale);
+            skip = !(norm < __builtin_inf());
+            if (a.norm_out && blockIdx.x == 0 && threadIdx.x == 0) *a.norm_out = (float)norm;
+            if (a.max_norm > 0.0 && norm > a.max_norm) s.scale = (float)(a.max_norm / (norm + 1e-6)) * s.scale;
+        }
+        lr = a.lr * (a.lr_factor ? (double)*a.lr_factor : 1.0);
+        s.b1 = (float)a.beta1;
+        s.b2 = (float)a.beta2;
+        s.c1 = (float)(1.0 - a.beta1);
+        s.c2 = (float)(1.0 - a.beta2);
+        s.eps = (float)a.eps;
+    };
+    for (int64_t u = blockIdx.x; u < a.units; u += gridDim.x) {
         const int k0 = units[u];
         const AdamTensor t = tensor_at(tensors + k0);
         const void* grad = grads[k0];
+        const int64_t unit_lo = (u - t.first_unit) * (K * kApart), lo = unit_lo + (threadIdx.x / kWave) * kAdamBlock;
+        const bool whole = unit_lo + K * kApart <= t.count;
+        Blocks<K, STREAM> in;
+        if (whole) in.load(t, grad, lo);
+        if (!ready) prepare();                   // the first unit's numbers are on their way meanwhile
+        if (skip) break;
         const double tlr = lr * t.lr_scale;
         s.rate = (float)(tlr * inv_bias1);
         s.keep = (float)(1.0 - tlr * t.weight_decay);
         s.key = (uint32_t)hash_fold(key, (uint64_t)t.index);
-        const int64_t unit_lo = (u - t.first_unit) * (K * 1024), lo = unit_lo + wave * kAdamBlock;
-        if (unit_lo + K * 1024 <= t.count) {
-            if (t.state_type == LEGEND_STATE_BLOCK) whole_blocks<K, true>(t, grad, s, lo, 1024);
-            else whole_blocks<K, false>(t, grad, s, lo, 1024);
+        if (whole) {
+            if (t.state_type == LEGEND_STATE_BLOCK) in.template finish<true>(t, s, lo);
+            else in.template finish<false>(t, s, lo);
         } else {
             for (int k = 0; k < K; ++k) {
-                const int64_t at = lo + k * 1024;
+                const int64_t at = lo + k * kApart;
                 if (at >= t.count) break;
-                if (at + kAdamBlock > t.count) part_block(t, grad, s, at);
-                else if (t.state_type == LEGEND_STATE_BLOCK) whole_blocks<1, true>(t, grad, s, at, 0);
-                else whole_blocks<1, false>(t, grad, s, at, 0);
+                if (at + kAdamBlock > t.count) {
+                    part_block(t, grad, s, at);
+                } else {
+                    Blocks<1, STREAM> one;
+                    one.load(t, grad, at);
+                    if (t.state_type == LEGEND_STATE_BLOCK) one.template finish<true>(t, s, at);
+                    else one.template finish<false>(t, s, at);
+                }
             }
         }
     }
+    if (!ready) prepare();                       // no units at all
 
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         AdamState& st = *a.state;
@@ -356,8 +426,8 @@ __global__ void __launch_bounds__(256) k_adamw(AdamParams a, int norm_parts) {
     }
 }
 
-// Small sets: units of 1024, so that more workgroups share them.  Large ones: 4096, so that a wave has four blocks' loads in flight.
-int adam_unit_elems(int64_t total) { return total >= kLargeTotal ? 4096 : 1024; }
+// Small sets: units of 1024, so that more workgroups share them.  Large ones: 2048, so that a wave has two blocks' loads in flight.
+int adam_unit_elems(int64_t total) { return total >= kLargeTotal ? KL * kApart : kApart; }
 
 void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2) {
     *s = AdamState{};
@@ -366,20 +436,21 @@ void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2) {
     s->power2 = std::pow(beta2, (double)(steps + 1));
 }
 
-template <int K>
+template <int K, bool STREAM>
 static hipError_t launch_units(hipStream_t st, const AdamParams& a) {
-    const int parts = (int)(a.units < kAdamNormParts ? a.units : kAdamNormParts);
+    const int parts = (int)(a.units < NP ? a.units : NP);
     if (a.with_norm && parts > 0) k_grad_squares<K><<<parts, 256, 0, st>>>(a);
     else k_begin_step<<<1, 1, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t grid = a.units < 1 ? 1 : (a.units < kStepGrid ? a.units : kStepGrid);
-    k_adamw<K><<<(unsigned)grid, 256, 0, st>>>(a, parts);
+    k_adamw<K, STREAM><<<(unsigned)grid, 256, 0, st>>>(a, parts);
     return hipGetLastError();
 }
 
 hipError_t launch_adamw(hipStream_t st, const AdamParams& a) {
-    return a.unit_elems == 4096 ? launch_units<4>(st, a) : launch_units<1>(st, a);
+    if (a.unit_elems == kApart) return launch_units<1, false>(st, a);
+    return a.stream ? launch_units<KL, true>(st, a) : launch_units<KL, false>(st, a);
 }
 
 }  // namespace legend

@@ -23,12 +23,13 @@ __device__ inline void load_quad(const T* p, float* out) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) out[j] = (float)v[j];
 }
-template <class T>
+template <bool STREAM = false, class T>
 __device__ inline void store_quad(T* p, const float* in) {
     typename Quad<T>::type v;
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = (T)in[j];
-    *reinterpret_cast<typename Quad<T>::type*>(p) = v;
+    if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<typename Quad<T>::type*>(p));
+    else *reinterpret_cast<typename Quad<T>::type*>(p) = v;
 }
 
 // one element of a tensor whose type is known at run time only
