@@ -17,14 +17,15 @@ constexpr float kTopCode = 448.f;           // largest e4m3 value
 constexpr float kLeastCode = 0.001953125f;  // smallest above zero, 2^-9
 constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100: 1 / scale stays far from infinity
 
-#ifndef KL
-#define KL 2
-#define LT (4 << 20)
-#define SG 2048
-#define NP 1024
-#endif
-constexpr int64_t kLargeTotal = LT;    // elements
-constexpr int64_t kStepGrid = SG;         // workgroups of a step: eight a compute unit
+// Sets of fewer elements are cut into units of 1024, so that more workgroups share them, and their workgroups all fit the card at a
+// time (five a compute unit by their registers); larger ones into units of 2048, two blocks in flight a wave (four: 344 against 333 us
+// for 60 M fp32 parameters, 515 against 417 for 120 M bf16 with 8-bit states: too many registers; units of 2048 for 3 M elements: 28.0
+// against 24.8).
+constexpr int64_t kLargeTotal = 4 << 20;
+constexpr int64_t kGridSmall = 1280, kGridLarge = 2048;      // workgroups of a step
+// of the kernel of the squares, each with a partial sum that every workgroup of a step adds up again (120 M elements: 2048 of them
+// read the gradients at 5 TB/s, 1024 at 3.6; 3 M: 24.7 against 25.5 us for the whole step)
+constexpr int kPartsSmall = 1024, kPartsLarge = kAdamNormParts;
 
 // Largest of the wave's numbers, none below zero, in all lanes.  Compared as integers, which orders them alike, with infinity and
 // NaN at the top.
@@ -426,8 +427,7 @@ __global__ void __launch_bounds__(256) k_adamw(AdamParams a, int norm_parts) {
     }
 }
 
-// Small sets: units of 1024, so that more workgroups share them.  Large ones: 2048, so that a wave has two blocks' loads in flight.
-int adam_unit_elems(int64_t total) { return total >= kLargeTotal ? KL * kApart : kApart; }
+int adam_unit_elems(int64_t total) { return total >= kLargeTotal ? 2 * kApart : kApart; }
 
 void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2) {
     *s = AdamState{};
@@ -438,19 +438,20 @@ void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2) {
 
 template <int K, bool STREAM>
 static hipError_t launch_units(hipStream_t st, const AdamParams& a) {
-    const int parts = (int)(a.units < NP ? a.units : NP);
+    const int64_t most_parts = K > 1 ? kPartsLarge : kPartsSmall, most = K > 1 ? kGridLarge : kGridSmall;
+    const int parts = (int)(a.units < most_parts ? a.units : most_parts);
     if (a.with_norm && parts > 0) k_grad_squares<K><<<parts, 256, 0, st>>>(a);
     else k_begin_step<<<1, 1, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t grid = a.units < 1 ? 1 : (a.units < kStepGrid ? a.units : kStepGrid);
+    const int64_t grid = a.units < 1 ? 1 : (a.units < most ? a.units : most);
     k_adamw<K, STREAM><<<(unsigned)grid, 256, 0, st>>>(a, parts);
     return hipGetLastError();
 }
 
 hipError_t launch_adamw(hipStream_t st, const AdamParams& a) {
     if (a.unit_elems == kApart) return launch_units<1, false>(st, a);
-    return a.stream ? launch_units<KL, true>(st, a) : launch_units<KL, false>(st, a);
+    return a.stream ? launch_units<2, true>(st, a) : launch_units<2, false>(st, a);
 }
 
 }  // namespace legend

@@ -11,9 +11,11 @@
 // to row.  Bound by HBM: an element is read and written once, for some ten vector instructions.
 #include "norm_rows.h"
 
+#include <type_traits>
+
 namespace legend {
 
-template <class XT, class YT, class S>
+template <class XT, class YT, class S, bool TABLE>
 __global__ void __launch_bounds__(S::threads) k_norm_forward(NormParams a) {
     constexpr int NE = S::NE, T = S::T, R = S::R;
     __shared__ float box[2][32];
@@ -23,17 +25,20 @@ __global__ void __launch_bounds__(S::threads) k_norm_forward(NormParams a) {
     const int64_t stride = (int64_t)gridDim.x * S::groups * R;
     RowColumns<XT, S> next[R];
     bool next_good[R];
+    RowSource<XT, TABLE, R> source;
     auto load = [&](int64_t r0) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const XT* src = r0 + i < a.rows ? source_row<XT>(a, r0 + i, lane == 0) : nullptr;
+            const XT* src = source.row(a, r0, i, lane == 0);
             next_good[i] = src != nullptr;
             if (src) next[i].load(src, d, lane);
             else next[i].clear();
         }
     };
     int64_t r0 = ((int64_t)blockIdx.x * S::groups + threadIdx.x / T) * R;
+    source.name(a, r0);
     load(r0);
+    source.name(a, r0 + stride);
     float w[NE], b[NE];
     load_parameter<S>(a.weight, a.weight_type, 1.f, d, lane, w);
     load_parameter<S>(a.bias, a.weight_type, 0.f, d, lane, b);
@@ -46,7 +51,10 @@ __global__ void __launch_bounds__(S::threads) k_norm_forward(NormParams a) {
 #pragma unroll
             for (int k = 0; k < NE; ++k) x[i][k] = S::inside(k, lane, d) ? next[i].number(k) : 0.f;
         }
-        if (r0 + stride < a.rows) load(r0 + stride);          // the next rows arrive while these are worked on
+        if (r0 + stride < a.rows) {                            // the next rows arrive while these are worked on
+            load(r0 + stride);
+            source.name(a, r0 + 2 * stride);
+        }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             if (r0 + i >= a.rows) continue;
@@ -93,14 +101,14 @@ __global__ void __launch_bounds__(S::threads) k_norm_forward(NormParams a) {
 
 template <class XT, class YT, bool Q>
 __global__ void __launch_bounds__(1024) k_norm_forward_long(NormParams a) {
-    typedef NormShape<16, 1024, 1, 0, Q> S;
+    typedef NormShape<16, 1024, 1, 0, Q, 1024> S;
     constexpr int NE = S::NE, PANEL = S::NE * S::T;
     __shared__ float box[2][32];
     int turn = 0;
     const int d = a.dim, lane = threadIdx.x;
     const float inv_d = 1.f / (float)d;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const XT* x = source_row<XT>(a, r, lane == 0);
+        const XT* x = static_cast<const XT*>(a.x) + r * a.x_stride;
         YT* y = static_cast<YT*>(a.y) + r * a.y_stride;
         float mean = 0.f, rstd = 0.f, left = 0.f, none = 0.f;
         float v[NE];
@@ -114,52 +122,46 @@ __global__ void __launch_bounds__(1024) k_norm_forward_long(NormParams a) {
                 f(at, d - at);
             }
         };
-        if (x) {
-            sweep(0.f, [&](int, int) {
+        sweep(0.f, [&](int, int) {
 #pragma unroll
-                for (int k = 0; k < NE; ++k) mean += v[k];
-            });
-            row_sum<1024, 1>(mean, none, box, turn);
-            mean *= inv_d;
-            float sq = 0.f;
-            sweep(mean, [&](int, int) {
+            for (int k = 0; k < NE; ++k) mean += v[k];
+        });
+        row_sum<1024, 1>(mean, none, box, turn);
+        mean *= inv_d;
+        float sq = 0.f;
+        sweep(mean, [&](int, int) {
+#pragma unroll
+            for (int k = 0; k < NE; ++k) {
+                left += v[k];
+                sq = fmaf(v[k], v[k], sq);
+            }
+        });
+        row_sum<1024, 2>(left, sq, box, turn);
+        left *= inv_d;
+        float var = sq * inv_d;
+        if (left * left > kLeftShare * var) {
+            sq = 0.f;
+            sweep(mean, [&](int, int n) {
 #pragma unroll
                 for (int k = 0; k < NE; ++k) {
-                    left += v[k];
-                    sq = fmaf(v[k], v[k], sq);
+                    const float c = S::inside(k, lane, n) ? v[k] - left : 0.f;
+                    sq = fmaf(c, c, sq);
                 }
             });
-            row_sum<1024, 2>(left, sq, box, turn);
-            left *= inv_d;
-            float var = sq * inv_d;
-            if (left * left > kLeftShare * var) {
-                sq = 0.f;
-                sweep(mean, [&](int, int n) {
-#pragma unroll
-                    for (int k = 0; k < NE; ++k) {
-                        const float c = S::inside(k, lane, n) ? v[k] - left : 0.f;
-                        sq = fmaf(c, c, sq);
-                    }
-                });
-                row_sum<1024, 1>(sq, none, box, turn);
-                var = sq * inv_d;
-            } else {
-                var = fmaf(-left, left, var);
-            }
-            rstd = 1.f / sqrtf(var + a.eps);
-            sweep(mean, [&](int at, int n) {
-                float w[NE], b[NE];
-                load_parameter<S>(a.weight, a.weight_type, 1.f, n, lane, w, at);
-                load_parameter<S>(a.bias, a.weight_type, 0.f, n, lane, b, at);
-#pragma unroll
-                for (int k = 0; k < NE; ++k) v[k] = fmaf((v[k] - left) * rstd, w[k], b[k]);
-                store_columns<S>(y + at, n, lane, v);
-            });
+            row_sum<1024, 1>(sq, none, box, turn);
+            var = sq * inv_d;
         } else {
-#pragma unroll
-            for (int k = 0; k < NE; ++k) v[k] = 0.f;
-            for (int at = 0; at < d; at += PANEL) store_columns<S>(y + at, d - at, lane, v);
+            var = fmaf(-left, left, var);
         }
+        rstd = 1.f / sqrtf(var + a.eps);
+        sweep(mean, [&](int at, int n) {
+            float w[NE], b[NE];
+            load_parameter<S>(a.weight, a.weight_type, 1.f, n, lane, w, at);
+            load_parameter<S>(a.bias, a.weight_type, 0.f, n, lane, b, at);
+#pragma unroll
+            for (int k = 0; k < NE; ++k) v[k] = fmaf((v[k] - left) * rstd, w[k], b[k]);
+            store_columns<S>(y + at, n, lane, v);
+        });
         if (lane == 0) {
             if (a.mean) a.mean[r] = mean + left;
             if (a.rstd) a.rstd[r] = rstd;
@@ -169,17 +171,22 @@ __global__ void __launch_bounds__(1024) k_norm_forward_long(NormParams a) {
 
 hipError_t launch_norm_forward(hipStream_t st, const NormParams& a) {
     if (a.rows <= 0) return hipSuccess;
+    if (a.status && a.dim > kTableRowMax) return hipErrorInvalidValue;
     return for_types(a.x_type, a.y_type, [&](auto xt, auto yt) {
+        typedef decltype(xt) XT;
+        typedef decltype(yt) YT;
         if (a.dim > kNormRowMax) {
             const unsigned grid = (unsigned)(a.rows < 512 ? a.rows : 512);
-            if (a.dim % 4 == 0) k_norm_forward_long<decltype(xt), decltype(yt), true><<<grid, 1024, 0, st>>>(a);
-            else k_norm_forward_long<decltype(xt), decltype(yt), false><<<grid, 1024, 0, st>>>(a);
+            if (a.dim % 4 == 0) k_norm_forward_long<XT, YT, true><<<grid, 1024, 0, st>>>(a);
+            else k_norm_forward_long<XT, YT, false><<<grid, 1024, 0, st>>>(a);
         } else {
-            for_shape<1>(a.dim, [&](auto s) {
+            for_shape<1, 256>(a.dim, [&](auto s) {
                 typedef decltype(s) S;
                 // at most the 2048 threads that a compute unit holds, so that weight and bias are loaded once a workgroup
                 const int64_t need = (a.rows + S::groups * S::R - 1) / (S::groups * S::R), most = 256 * 2048 / S::threads;
-                k_norm_forward<decltype(xt), decltype(yt), S><<<(unsigned)(need < most ? need : most), S::threads, 0, st>>>(a);
+                const unsigned grid = (unsigned)(need < most ? need : most);
+                if (!a.status) k_norm_forward<XT, YT, S, false><<<grid, S::threads, 0, st>>>(a);
+                else if constexpr (std::is_same<XT, float>::value && S::LOW < kTableRowMax) k_norm_forward<XT, YT, S, true><<<grid, S::threads, 0, st>>>(a);
                 return 0;
             });
         }

@@ -7,14 +7,16 @@
 // atomics: the same bits every time).  Bound by HBM.
 #include "norm_rows.h"
 
+#include <type_traits>
+
 namespace legend {
 
-template <class XT, class YT, class S>
+template <class XT, class YT, class S, bool TABLE>
 __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     constexpr int NE = S::NE, T = S::T, R = S::R, G = S::groups;
     constexpr bool KEEP = NE < 32;               // the weight in registers; longer rows read it again for every row (from L2)
     __shared__ float box[2][32];
-    __shared__ float sums[G > 1 ? 2 * 256 * NE : 1];
+    __shared__ float sums[G > 1 ? 2 * S::threads * NE : 1];
     int turn = 0;
     const int d = a.dim, lane = threadIdx.x % T;
     const float inv_d = 1.f / (float)d;
@@ -22,10 +24,11 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     RowColumns<XT, S> next_x[R];
     RowColumns<YT, S> next_g[R];
     float next_mean[R], next_rstd[R];
+    RowSource<XT, TABLE, R> source;
     auto load = [&](int64_t r0) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const XT* src = r0 + i < a.rows ? source_row<XT>(a, r0 + i, lane == 0) : nullptr;
+            const XT* src = source.row(a, r0, i, lane == 0);
             next_mean[i] = next_rstd[i] = 0.f;
             if (src) {
                 next_x[i].load(src, d, lane);
@@ -39,7 +42,9 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
         }
     };
     int64_t r0 = ((int64_t)blockIdx.x * G + threadIdx.x / T) * R;
+    source.name(a, r0);
     load(r0);
+    source.name(a, r0 + stride);
     float w[NE], dw[NE], db[NE];
     if (KEEP) load_parameter<S>(a.weight, a.weight_type, 1.f, d, lane, w);
 #pragma unroll
@@ -57,7 +62,10 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
             }
         }
         if (!KEEP) load_parameter<S>(a.weight, a.weight_type, 1.f, d, lane, w);
-        if (r0 + stride < a.rows) load(r0 + stride);          // the next rows arrive while these are worked on
+        if (r0 + stride < a.rows) {                            // the next rows arrive while these are worked on
+            load(r0 + stride);
+            source.name(a, r0 + 2 * stride);
+        }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             if (r0 + i >= a.rows) continue;
@@ -106,7 +114,7 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
 
 template <class XT, class YT, bool Q>
 __global__ void __launch_bounds__(1024) k_norm_backward_long(NormParams a) {
-    typedef NormShape<16, 1024, 1, 0, Q> S;
+    typedef NormShape<16, 1024, 1, 0, Q, 1024> S;
     constexpr int NE = S::NE, PANEL = S::NE * S::T;
     __shared__ float box[2][32];
     int turn = 0;
@@ -117,15 +125,9 @@ __global__ void __launch_bounds__(1024) k_norm_backward_long(NormParams a) {
     bool first = true;
     float xh[NE], g[NE], w[NE];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const XT* x = source_row<XT>(a, r, lane == 0);
+        const XT* x = static_cast<const XT*>(a.x) + r * a.x_stride;
         const YT* dy = static_cast<const YT*>(a.dy) + r * a.dy_stride;
         XT* dx = a.dx ? static_cast<XT*>(a.dx) + r * a.dx_stride : nullptr;
-        if (!x) {
-#pragma unroll
-            for (int k = 0; k < NE; ++k) g[k] = 0.f;
-            if (dx) for (int at = 0; at < d; at += PANEL) store_columns<S>(dx + at, d - at, lane, g);
-            continue;
-        }
         const float mean = a.mean[r], rstd = a.rstd[r];
         auto take = [&](int at) {
             RowColumns<XT, S> px;
@@ -215,27 +217,31 @@ __global__ void __launch_bounds__(1024) k_norm_sums(NormParams a) {
 int norm_parts(int64_t rows, int32_t dim) {
     int64_t need = rows, most = 256;
     if (dim <= kNormRowMax)
-        for_shape<2>(dim, [&](auto s) {
+        for_shape<2, 512>(dim, [&](auto s) {
             typedef decltype(s) S;
             need = (rows + S::groups * S::R - 1) / (S::groups * S::R);
-            if (S::threads <= 256) most = 512;
+            if (S::T <= 256) most = 512;
             return 0;
         });
     return (int)(need < most ? need : most);
 }
 
 hipError_t launch_norm_backward(hipStream_t st, const NormParams& a) {
+    if (a.rows > 0 && a.status && a.dim > kTableRowMax) return hipErrorInvalidValue;
     if (a.rows > 0) {
         hipError_t e = for_types(a.x_type, a.dy_type, [&](auto xt, auto yt) {
+            typedef decltype(xt) XT;
+            typedef decltype(yt) YT;
             if (a.dim > kNormRowMax) {
-                if (a.dim % 4 == 0) k_norm_backward_long<decltype(xt), decltype(yt), true><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
-                else k_norm_backward_long<decltype(xt), decltype(yt), false><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
+                if (a.dim % 4 == 0) k_norm_backward_long<XT, YT, true><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
+                else k_norm_backward_long<XT, YT, false><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
             } else {
-                for_shape<2>(a.dim, [&](auto s) {
+                for_shape<2, 512>(a.dim, [&](auto s) {
                     typedef decltype(s) S;
                     const int64_t need = (a.rows + S::groups * S::R - 1) / (S::groups * S::R), most = 256 * 2048 / S::threads;
                     const unsigned grid = a.partial ? (unsigned)a.parts : (unsigned)(need < most ? need : most);
-                    k_norm_backward<decltype(xt), decltype(yt), S><<<grid, S::threads, 0, st>>>(a);
+                    if (!a.status) k_norm_backward<XT, YT, S, false><<<grid, S::threads, 0, st>>>(a);
+                    else if constexpr (std::is_same<XT, float>::value && S::LOW < kTableRowMax) k_norm_backward<XT, YT, S, true><<<grid, S::threads, 0, st>>>(a);
                     return 0;
                 });
             }

@@ -228,7 +228,7 @@ hipError_t launch_norm_forward(hipStream_t st, const NormParams& a);
 hipError_t launch_norm_backward(hipStream_t st, const NormParams& a);
 
 constexpr int kAdamBlock = 256;             // elements that share a scale
-constexpr int kAdamNormParts = 1024;        // partial sums of the gradient norm
+constexpr int kAdamNormParts = 2048;        // partial sums of the gradient norm
 struct AdamTensor {
     void* param; float* master; void* m; void* v; float* m_scale; float* v_scale;
     int64_t count, first_unit;

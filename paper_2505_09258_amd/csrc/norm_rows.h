@@ -9,16 +9,13 @@ namespace legend {
 
 constexpr float kLeftShare = 9.765625e-4f;   // 2^-10: the difference then loses a thousandth of a bit
 
-// Address of row r, or null (and its bit in *status) for a row of a table that the call may not read.
-template <class XT>
-__device__ inline const XT* source_row(const NormParams& a, int64_t r, bool reports) {
-    if (!a.status) return static_cast<const XT*>(a.x) + r * a.x_stride;
-    const int64_t id = a.ids ? a.ids[r] : r;
+// A row of a table by its id, or null (and its bit in *status) for one that the call may not read.
+__device__ inline const float* table_row(const NormParams& a, int64_t id, bool reports) {
     if (id < 0 || id >= a.table_rows) {
         if (reports) atomicOr(a.status, 1u);
         return nullptr;
     }
-    if (a.rel_base) return reinterpret_cast<const XT*>(a.rel_base + id * a.dim);
+    if (a.rel_base) return a.rel_base + id * a.dim;
     // (a 64-bit division takes ten times the instructions of a 32-bit one)
     const int64_t p = a.table_rows <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)a.rows_per_partition) : id / a.rows_per_partition;
     const float* base = a.part_base[p];
@@ -26,8 +23,25 @@ __device__ inline const XT* source_row(const NormParams& a, int64_t r, bool repo
         if (reports) atomicOr(a.status, 2u);
         return nullptr;
     }
-    return reinterpret_cast<const XT*>(base + (id - p * a.rows_per_partition) * a.dim);
+    return base + (id - p * a.rows_per_partition) * a.dim;
 }
+
+// The rows of a call, R at a time, as the kernels ask for them: of a table, the ids a turn ahead of the rows that they name.
+template <class XT, bool TABLE, int R>
+struct RowSource {
+    int64_t id[R];
+    __device__ void name(const NormParams& a, int64_t r0) {
+        if (!TABLE) return;
+#pragma unroll
+        for (int i = 0; i < R; ++i) id[i] = a.ids && r0 + i < a.rows ? a.ids[r0 + i] : r0 + i;
+    }
+    // row r0 + i of the named ones; null behind the last row too
+    __device__ const XT* row(const NormParams& a, int64_t r0, int i, bool reports) const {
+        if (r0 + i >= a.rows) return nullptr;
+        if (!TABLE) return static_cast<const XT*>(a.x) + (r0 + i) * a.x_stride;
+        return reinterpret_cast<const XT*>(table_row(a, id[i], reports));
+    }
+};
 
 template <int CTRL>
 __device__ inline float dpp_move(float v) {
@@ -80,11 +94,11 @@ __device__ inline void row_sum(float& p, float& q, float (*box)[32], int& turn) 
 // How a row is dealt to threads: NE columns a thread, T threads a row, R rows at a time, rows of more than LOW columns.  Q:
 // groups of four columns (16- or 8-byte accesses at any address), for dimensions that are a multiple of four; otherwise single columns,
 // neighbours in neighbouring threads.
-template <int NE_, int T_, int R_, int LOW_, bool Q_>
+template <int NE_, int T_, int R_, int LOW_, bool Q_, int WG_>
 struct NormShape {
     static constexpr int NE = NE_, T = T_, R = R_, LOW = LOW_;
     static constexpr bool Q = Q_;
-    static constexpr int threads = T_ < 256 ? 256 : T_;      // of a workgroup
+    static constexpr int threads = T_ < WG_ ? WG_ : T_;      // of a workgroup
     static constexpr int groups = threads / T_;              // rows that a workgroup holds at a time, R times over
     static __device__ int column(int k, int lane) { return Q ? (k >> 2) * (4 * T) + lane * 4 + (k & 3) : k * T + lane; }
     // first column of the access that column k belongs to, and whether it lies in the row (always, below LOW)
@@ -93,24 +107,25 @@ struct NormShape {
         return (Q ? ((k >> 2) + 1) * (4 * T) : (k + 1) * T) <= LOW || access(k, lane) < dim;
     }
 };
+constexpr int kTableRowMax = 512;            // columns of a table's rows at most
 constexpr int kNormRowMax = 16384;           // longer rows do not fit a workgroup's registers
 
-// R: rows of at most 512 columns that a thread group takes at a time
-template <int R, bool Q, class F>
+// R: rows of at most 512 columns that a thread group takes at a time; WG: threads of a workgroup where a row needs no more than a wave
+template <int R, int WG, bool Q, class F>
 auto for_columns(int dim, F&& f) {
-    if (dim <= 32) return f(NormShape<4, 8, R, 0, Q>{});
-    if (dim <= 64) return f(NormShape<4, 16, R, 32, Q>{});
-    if (dim <= 128) return f(NormShape<4, 32, R, 64, Q>{});
-    if (dim <= 256) return f(NormShape<4, 64, R, 128, Q>{});
-    if (dim <= 512) return f(NormShape<8, 64, R, 256, Q>{});
-    if (dim <= 1024) return f(NormShape<16, 64, 1, 512, Q>{});
-    if (dim <= 2048) return f(NormShape<8, 256, 1, 1024, Q>{});
-    if (dim <= 4096) return f(NormShape<16, 256, 1, 2048, Q>{});
-    if (dim <= 8192) return f(NormShape<16, 512, 1, 4096, Q>{});
-    return f(NormShape<32, 512, 1, 8192, Q>{});
+    if (dim <= 32) return f(NormShape<4, 8, R, 0, Q, WG>{});
+    if (dim <= 64) return f(NormShape<4, 16, R, 32, Q, WG>{});
+    if (dim <= 128) return f(NormShape<4, 32, R, 64, Q, WG>{});
+    if (dim <= 256) return f(NormShape<4, 64, R, 128, Q, WG>{});
+    if (dim <= 512) return f(NormShape<8, 64, R, 256, Q, WG>{});
+    if (dim <= 1024) return f(NormShape<16, 64, 1, 512, Q, WG>{});
+    if (dim <= 2048) return f(NormShape<8, 256, 1, 1024, Q, 256>{});
+    if (dim <= 4096) return f(NormShape<16, 256, 1, 2048, Q, 256>{});
+    if (dim <= 8192) return f(NormShape<16, 512, 1, 4096, Q, 512>{});
+    return f(NormShape<32, 512, 1, 8192, Q, 512>{});
 }
-template <int R, class F>
-auto for_shape(int dim, F&& f) { return dim % 4 == 0 ? for_columns<R, true>(dim, f) : for_columns<R, false>(dim, f); }
+template <int R, int WG, class F>
+auto for_shape(int dim, F&& f) { return dim % 4 == 0 ? for_columns<R, WG, true>(dim, f) : for_columns<R, WG, false>(dim, f); }
 
 // A thread's columns of a row as they lie in memory.  Accesses behind the row's end read its last columns instead: no branch
 // between the loads; `inside` says which numbers count.
