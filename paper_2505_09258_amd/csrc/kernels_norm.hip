@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(S::threads) k_norm_forward(NormParams a) {
 
 // ---- rows that do not fit a workgroup's registers: 16384 columns at a time, read again for every sweep ----------------
 
-template <class XT, class YT, bool Q>
+template <class XT, class YT, NormColumns Q>
 __global__ void __launch_bounds__(1024) k_norm_forward_long(NormParams a) {
     typedef NormShape<16, 1024, 1, 0, Q, 1024> S;
     constexpr int NE = S::NE, PANEL = S::NE * S::T;
@@ -177,8 +177,8 @@ hipError_t launch_norm_forward(hipStream_t st, const NormParams& a) {
         typedef decltype(yt) YT;
         if (a.dim > kNormRowMax) {
             const unsigned grid = (unsigned)(a.rows < 512 ? a.rows : 512);
-            if (a.dim % 4 == 0) k_norm_forward_long<XT, YT, true><<<grid, 1024, 0, st>>>(a);
-            else k_norm_forward_long<XT, YT, false><<<grid, 1024, 0, st>>>(a);
+            if (a.dim % 4 == 0) k_norm_forward_long<XT, YT, QUADS><<<grid, 1024, 0, st>>>(a);
+            else k_norm_forward_long<XT, YT, RAGGED><<<grid, 1024, 0, st>>>(a);
         } else {
             for_shape<1, 256>(a.dim, [&](auto s) {
                 typedef decltype(s) S;

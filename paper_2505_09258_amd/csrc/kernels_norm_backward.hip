@@ -97,8 +97,9 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     float* mine = sums + (threadIdx.x / T) * (2 * T * NE);
 #pragma unroll
     for (int k = 0; k < NE; ++k) {
-        mine[S::column(k, lane)] = dw[k];
-        mine[T * NE + S::column(k, lane)] = db[k];
+        if (!S::inside(k, lane, d)) continue;
+        mine[S::column(k, lane, d)] = dw[k];
+        mine[T * NE + S::column(k, lane, d)] = db[k];
     }
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * T * NE; c += S::threads) {
@@ -112,7 +113,7 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
 
 // ---- rows that do not fit a workgroup's registers: 16384 columns at a time ---------------------------------------------
 
-template <class XT, class YT, bool Q>
+template <class XT, class YT, NormColumns Q>
 __global__ void __launch_bounds__(1024) k_norm_backward_long(NormParams a) {
     typedef NormShape<16, 1024, 1, 0, Q, 1024> S;
     constexpr int NE = S::NE, PANEL = S::NE * S::T;
@@ -233,8 +234,8 @@ hipError_t launch_norm_backward(hipStream_t st, const NormParams& a) {
             typedef decltype(xt) XT;
             typedef decltype(yt) YT;
             if (a.dim > kNormRowMax) {
-                if (a.dim % 4 == 0) k_norm_backward_long<XT, YT, true><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
-                else k_norm_backward_long<XT, YT, false><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
+                if (a.dim % 4 == 0) k_norm_backward_long<XT, YT, QUADS><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
+                else k_norm_backward_long<XT, YT, RAGGED><<<norm_parts(a.rows, a.dim), 1024, 0, st>>>(a);
             } else {
                 for_shape<2, 512>(a.dim, [&](auto s) {
                     typedef decltype(s) S;

@@ -91,27 +91,38 @@ __device__ inline void row_sum(float& p, float& q, float (*box)[32], int& turn) 
     for (int k = 1; k < W; ++k) q += b[16 + k];
 }
 
-// How a row is dealt to threads: NE columns a thread, T threads a row, R rows at a time, rows of more than LOW columns.  Q:
-// groups of four columns (16- or 8-byte accesses at any address), for dimensions that are a multiple of four; otherwise single columns,
-// neighbours in neighbouring threads.
-template <int NE_, int T_, int R_, int LOW_, bool Q_, int WG_>
+// How a row is dealt to threads: NE columns a thread, T threads a row, R rows at a time, rows of more than LOW columns, WG threads a
+// workgroup at least.  Columns go in groups of four, one 16- or 8-byte access at whatever address.  QUADS: dimensions that are a
+// multiple of four; accesses behind the row's end go to its last four columns instead and count for nothing.  RAGGED: the others;
+// the group that holds the row's end reads the row's last four columns too, and only those count that are no other group's.
+// SINGLE: fewer than four columns, one by one.
+enum NormColumns { QUADS, RAGGED, SINGLE };
+template <int NE_, int T_, int R_, int LOW_, NormColumns MODE_, int WG_>
 struct NormShape {
     static constexpr int NE = NE_, T = T_, R = R_, LOW = LOW_;
-    static constexpr bool Q = Q_;
+    static constexpr NormColumns MODE = MODE_;
     static constexpr int threads = T_ < WG_ ? WG_ : T_;      // of a workgroup
     static constexpr int groups = threads / T_;              // rows that a workgroup holds at a time, R times over
-    static __device__ int column(int k, int lane) { return Q ? (k >> 2) * (4 * T) + lane * 4 + (k & 3) : k * T + lane; }
-    // first column of the access that column k belongs to, and whether it lies in the row (always, below LOW)
-    static __device__ int access(int k, int lane) { return Q ? (k >> 2) * (4 * T) + lane * 4 : k * T + lane; }
+    // the group of four that number k of a thread belongs to: the first column that is its own, and the first that it reads
+    static __device__ int own(int k, int lane) { return MODE == SINGLE ? k * T + lane : (k >> 2) * (4 * T) + lane * 4; }
+    static __device__ int first(int k, int lane, int dim) {
+        const int c = own(k, lane), last = MODE == SINGLE ? dim - 1 : dim - 4;
+        return always(k) || c < last ? c : last;
+    }
+    static __device__ int column(int k, int lane, int dim) { return first(k, lane, dim) + (MODE == SINGLE ? 0 : k & 3); }
+    // every thread's number k lies in the row, whatever its dimension
+    static constexpr __device__ bool always(int k) { return MODE == SINGLE ? (k + 1) * T <= LOW : ((k >> 2) + 1) * (4 * T) <= LOW; }
     static __device__ bool inside(int k, int lane, int dim) {
-        return (Q ? ((k >> 2) + 1) * (4 * T) : (k + 1) * T) <= LOW || access(k, lane) < dim;
+        if (always(k)) return true;
+        if (MODE == RAGGED) return (k & 3) >= own(k, lane) - (dim - 4) || own(k, lane) <= dim - 4;
+        return own(k, lane) < dim;
     }
 };
 constexpr int kTableRowMax = 512;            // columns of a table's rows at most
 constexpr int kNormRowMax = 16384;           // longer rows do not fit a workgroup's registers
 
 // R: rows of at most 512 columns that a thread group takes at a time; WG: threads of a workgroup where a row needs no more than a wave
-template <int R, int WG, bool Q, class F>
+template <int R, int WG, NormColumns Q, class F>
 auto for_columns(int dim, F&& f) {
     if (dim <= 32) return f(NormShape<4, 8, R, 0, Q, WG>{});
     if (dim <= 64) return f(NormShape<4, 16, R, 32, Q, WG>{});
@@ -125,27 +136,23 @@ auto for_columns(int dim, F&& f) {
     return f(NormShape<32, 512, 1, 8192, Q, 512>{});
 }
 template <int R, int WG, class F>
-auto for_shape(int dim, F&& f) { return dim % 4 == 0 ? for_columns<R, WG, true>(dim, f) : for_columns<R, WG, false>(dim, f); }
+auto for_shape(int dim, F&& f) {
+    if (dim < 4) return f(NormShape<4, 8, R, 0, SINGLE, WG>{});
+    return dim % 4 == 0 ? for_columns<R, WG, QUADS>(dim, f) : for_columns<R, WG, RAGGED>(dim, f);
+}
 
-// A thread's columns of a row as they lie in memory.  Accesses behind the row's end read its last columns instead: no branch
-// between the loads; `inside` says which numbers count.
+// A thread's columns of a row as they lie in memory; no branch between the loads.  `inside` says which numbers count.
 template <class E, class S>
 struct RowColumns {
     typedef E quad __attribute__((ext_vector_type(4)));
     quad v[S::NE / 4];
     __device__ void load(const E* row, int dim, int lane) {
-        if (S::Q) {
+        if (S::MODE != SINGLE) {
 #pragma unroll
-            for (int k = 0; k < S::NE; k += 4) {
-                const int c = S::access(k, lane);
-                v[k / 4] = *reinterpret_cast<const typename Quad<E>::type*>(row + (S::inside(k, lane, dim) ? c : dim - 4));
-            }
+            for (int k = 0; k < S::NE; k += 4) v[k / 4] = *reinterpret_cast<const typename Quad<E>::type*>(row + S::first(k, lane, dim));
         } else {
 #pragma unroll
-            for (int k = 0; k < S::NE; ++k) {
-                const int c = S::access(k, lane);
-                v[k / 4][k % 4] = row[S::inside(k, lane, dim) ? c : dim - 1];
-            }
+            for (int k = 0; k < S::NE; ++k) v[k / 4][k % 4] = row[S::first(k, lane, dim)];
         }
     }
     __device__ void clear() {
@@ -157,14 +164,22 @@ struct RowColumns {
 
 template <class S, class E>
 __device__ inline void store_columns(E* row, int dim, int lane, const float* in) {
-    if (S::Q) {
+    if (S::MODE != SINGLE) {
 #pragma unroll
-        for (int k = 0; k < S::NE; k += 4)
-            if (S::inside(k, lane, dim)) store_quad(row + S::access(k, lane), in + k);
+        for (int k = 0; k < S::NE; k += 4) {
+            const int c = S::own(k, lane);
+            if (S::always(k) || c <= dim - 4) {
+                store_quad(row + c, in + k);
+            } else if (S::MODE == RAGGED && c < dim) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (S::inside(k + j, lane, dim)) row[S::column(k + j, lane, dim)] = (E)in[k + j];
+            }
+        }
     } else {
 #pragma unroll
         for (int k = 0; k < S::NE; ++k)
-            if (S::inside(k, lane, dim)) row[S::access(k, lane)] = (E)in[k];
+            if (S::inside(k, lane, dim)) row[S::column(k, lane, dim)] = (E)in[k];
     }
 }
 
