@@ -14,9 +14,11 @@ namespace legend {
 template <class XT, class YT, class S, bool TABLE>
 __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     constexpr int NE = S::NE, T = S::T, R = S::R, G = S::groups;
-    constexpr bool KEEP = NE < 32;               // the weight in registers; longer rows read it again for every row (from L2)
+    // The weight and the columns' sums in registers; for the longest rows the weight is read again for every row (from L2) and the
+    // sums lie in LDS (128 KB), each thread's in a place of its own.
+    constexpr bool KEEP = NE < 32;
     __shared__ float box[2][32];
-    __shared__ float sums[G > 1 ? 2 * S::threads * NE : 1];
+    __shared__ __align__(16) float sums[G > 1 || !KEEP ? 2 * S::threads * NE : 4];
     int turn = 0;
     const int d = a.dim, lane = threadIdx.x % T;
     const float inv_d = 1.f / (float)d;
@@ -45,10 +47,15 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     source.name(a, r0);
     load(r0);
     source.name(a, r0 + stride);
-    float w[NE], dw[NE], db[NE];
+    float w[NE], dw[KEEP ? NE : 1], db[KEEP ? NE : 1];
+    float4* far_w = reinterpret_cast<float4*>(sums) + threadIdx.x;             // !KEEP: this thread's sums, S::threads apart
+    float4* far_b = far_w + S::threads * (NE / 4);
     if (KEEP) load_parameter<S>(a.weight, a.weight_type, 1.f, d, lane, w);
 #pragma unroll
-    for (int k = 0; k < NE; ++k) dw[k] = db[k] = 0.f;
+    for (int k = 0; k < NE; ++k) {
+        if (KEEP) dw[k] = db[k] = 0.f;
+        else if (k % 4 == 0) far_w[k / 4 * S::threads] = far_b[k / 4 * S::threads] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
     for (; r0 < a.rows; r0 += stride) {
         float x[R][NE], g[R][NE], rstd[R];
 #pragma unroll
@@ -70,10 +77,25 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
         for (int i = 0; i < R; ++i) {
             if (r0 + i >= a.rows) continue;
             float su = 0.f, sx = 0.f;
+            if (!KEEP && a.partial) {
+#pragma unroll
+                for (int k = 0; k < NE; k += 4) {
+                    float4 p = far_w[k / 4 * S::threads], q = far_b[k / 4 * S::threads];
+                    p.x = fmaf(g[i][k], x[i][k], p.x);
+                    p.y = fmaf(g[i][k + 1], x[i][k + 1], p.y);
+                    p.z = fmaf(g[i][k + 2], x[i][k + 2], p.z);
+                    p.w = fmaf(g[i][k + 3], x[i][k + 3], p.w);
+                    q.x += g[i][k]; q.y += g[i][k + 1]; q.z += g[i][k + 2]; q.w += g[i][k + 3];
+                    far_w[k / 4 * S::threads] = p;
+                    far_b[k / 4 * S::threads] = q;
+                }
+            }
 #pragma unroll
             for (int k = 0; k < NE; ++k) {
-                dw[k] = fmaf(g[i][k], x[i][k], dw[k]);
-                db[k] += g[i][k];
+                if (KEEP) {
+                    dw[k] = fmaf(g[i][k], x[i][k], dw[k]);
+                    db[k] += g[i][k];
+                }
                 g[i][k] *= w[k];
                 su += g[i][k];
                 sx = fmaf(g[i][k], x[i][k], sx);
@@ -89,6 +111,16 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     }
     if (!a.partial) return;
     float* out = a.partial + (int64_t)blockIdx.x * 2 * d;
+    if (!KEEP) {
+        float t[NE];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int k = 0; k < NE; k += 4) *reinterpret_cast<float4*>(t + k) = (half ? far_b : far_w)[k / 4 * S::threads];
+            store_columns<S>(out + half * d, d, lane, t);
+        }
+        return;
+    }
     if (G == 1) {
         store_columns<S>(out, d, lane, dw);
         store_columns<S>(out + d, d, lane, db);
@@ -98,8 +130,8 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
 #pragma unroll
     for (int k = 0; k < NE; ++k) {
         if (!S::inside(k, lane, d)) continue;
-        mine[S::column(k, lane, d)] = dw[k];
-        mine[T * NE + S::column(k, lane, d)] = db[k];
+        mine[S::column(k, lane, d)] = dw[KEEP ? k : 0];
+        mine[T * NE + S::column(k, lane, d)] = db[KEEP ? k : 0];
     }
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * T * NE; c += S::threads) {
