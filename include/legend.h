@@ -451,7 +451,8 @@ int64_t legend_layer_norm_workspace(int64_t rows, int32_t dim);
  *   norm = *grad_scale * sqrt(sum of grad^2 over all tensors)  (64 bits),
  *   clip = max_norm > 0 and norm > max_norm ? max_norm / (norm + 1e-6) : 1.
  * With max_norm > 0 or a norm output asked for, a step whose norm is not finite changes nothing and counts as skipped.
- * Without both the norm is not computed and such gradients go through the formulas.  The root of a v below 2^-126 is 0.
+ * Without both the norm is not computed and such gradients go through the formulas.  The root of a v below 2^-126
+ * counts as some number below 2^-62; with 8-bit states, a v beyond fp32 makes its element NaN.
  * The number of steps lives on the device, so that a recorded step replays as the next one.
  *
  * States: LEGEND_STATE_FLOAT: m, v [count] fp32.  LEGEND_STATE_BLOCK: 8 bits; m and v hold m and sqrt(v) as e4m3 codes (1 sign, 4

@@ -16,6 +16,7 @@ namespace legend {
 constexpr float kTopCode = 448.f;           // largest e4m3 value
 constexpr float kLeastCode = 0.001953125f;  // smallest above zero, 2^-9
 constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100: 1 / scale stays far from infinity
+constexpr float kLeastNormal = 1.17549435e-38f;
 
 // Sets of fewer elements are cut into units of 1024, so that more workgroups share them, and their workgroups all fit the card at a
 // time (five a compute unit by their registers); larger ones into units of 2048, two blocks in flight a wave (four: 344 against 333 us
@@ -116,53 +117,95 @@ __device__ inline void codes_to_numbers(uint32_t codes, float scale, float* out)
     out[0] = lo[0] * scale; out[1] = lo[1] * scale; out[2] = hi[0] * scale; out[3] = hi[1] * scale;
 }
 
-// Moments and parameter of one element; the root of the new second moment comes back.  Root and reciprocal are the hardware's, each
-// within 1.6 half steps of fp32; a second moment below fp32's normal numbers has the root 0.
-__device__ inline float step_element(const Step& s, float g, float& m, float& v, float& p) {
+// The step of a parameter from its new moments; the reciprocal is the hardware's, within 1.6 half steps of fp32.
+__device__ inline float step_parameter(const Step& s, float m, float root, float p) {
+    const float down = m * __builtin_amdgcn_rcpf(fmaf(root, s.inv_bias2_root, s.eps));
+    return fmaf(p, s.keep, -(s.rate * down));
+}
+// 32-bit states: the hardware's root, within 1.6 half steps; a second moment below fp32's normal numbers has the root 0.
+__device__ inline void step_float(const Step& s, float g, float& m, float& v, float& p) {
     g *= s.scale;
     m = fmaf(s.b1, m, s.c1 * g);
     v = fmaf(s.b2, v, (s.c2 * g) * g);
-    const float root = __builtin_amdgcn_sqrtf(v);
-    const float down = m * __builtin_amdgcn_rcpf(fmaf(root, s.inv_bias2_root, s.eps));
-    p = fmaf(p, s.keep, -(s.rate * down));
-    return root;
+    p = step_parameter(s, m, __builtin_amdgcn_sqrtf(v), p);
 }
 
-// Scale of a block from its lanes' largest magnitudes v[0..3], and how many scales a number is: 2^-21 less than the reciprocal
-// says, so that the largest is never above the largest code.  Infinities and NaN do not count.
-__device__ inline float block_scale(const float* v, float& per_scale) {
-    float top = wave_max(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+// 8-bit states: every operation up to the code is rounded to nearest once, as it is written (a code depends on the last bit of
+// what it is made from: a root or a quotient that is a bit off is another code once in a million).
+// Root of v: from the hardware's reciprocal root by one step whose residual is exact.  NaN for infinity.
+__device__ inline float rounded_root(float v) {
+    const float c = fmaxf(v, kLeastNormal);
+    const float y = __builtin_amdgcn_rsqf(c);
+    const float q = c * y;
+    const float root = fmaf(fmaf(-q, q, c), 0.5f * y, q);
+    return v > 0.f ? root : v;
+}
+// a / b from y = 1 / b rounded to nearest
+__device__ inline float rounded_quotient(float a, float b, float y) {
+    const float q = a * y;
+    return fmaf(fmaf(-q, b, a), y, q);
+}
+__device__ inline void step_block(const Step& s, float g, float& m, float& v, float& root, float& p) {
+    g *= s.scale;
+    const float m0 = s.b1 * m, m1 = s.c1 * g;
+    m = m0 + m1;
+    const float v0 = s.b2 * v, v1 = (s.c2 * g) * g;
+    v = v0 + v1;
+    root = rounded_root(v);
+    p = step_parameter(s, m, root, p);
+}
+
+// Largest finite magnitude of a wave's numbers, and whether some are not finite.
+__device__ inline float block_top(const float* v, bool& odd) {
+    float top = wave_max(__uint_as_float(max(max(__float_as_uint(fabsf(v[0])), __float_as_uint(fabsf(v[1]))),
+                                             max(__float_as_uint(fabsf(v[2])), __float_as_uint(fabsf(v[3]))))));
     if (!(top < __builtin_inff())) {
+        odd = true;
         float t = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) t = fabsf(v[j]) < __builtin_inff() ? fmaxf(t, fabsf(v[j])) : t;
         top = wave_max(t);
     }
-    float s = top * (1.f / kTopCode);
-    s = s > kLeastScale ? s : 0.f;
-    per_scale = s > 0.f ? __builtin_amdgcn_rcpf(s) * (1.f - 4.76837158203125e-7f) : 0.f;
-    return s;
+    return top;
 }
-// The e4m3 codes of four first moments and roots.  The conversion adds a word's upper 20 bits below the last bit that it keeps, and
-// gives the NaN code for an infinity.
-__device__ inline void codes_of(const float* m, float m_per, const float* root, float root_per, const uint32_t* words, uint32_t& cm, uint32_t& cr) {
-    float x[4];
+struct Scale {
+    float s, y;                              // the scale and its reciprocal; both 0 where everything is
+};
+__device__ inline Scale scale_of(float top) {
+    const float s = top * (1.f / kTopCode);
+    const float y0 = __builtin_amdgcn_rcpf(s), y = fmaf(fmaf(-s, y0, 1.f), y0, y0);
+    return s > kLeastScale ? Scale{s, y} : Scale{0.f, 0.f};
+}
+// A block's scales and codes from its moments: me and ve, root the roots of ve.  The conversion adds a word's upper 20 bits below the
+// last bit that it keeps.
+__device__ inline void codes_of(const float* me, const float* ve, const float* root, const uint32_t* words, uint32_t& cm, uint32_t& cr, float& ms, float& vs) {
+    bool odd = false;
+    const float top_m = block_top(me, odd), top_v = block_top(ve, odd);
+    const Scale a = scale_of(top_m), b = scale_of(rounded_root(top_v));
+    ms = a.s;
+    vs = b.s;
+    float x[4], y[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        x[j] = root[j] * root_per;
-        x[j] = x[j] > 0.f ? fmaxf(x[j], kLeastCode) : x[j];
+        x[j] = __builtin_amdgcn_fmed3f(rounded_quotient(me[j], a.s, a.y), -kTopCode, kTopCode);
+        const float q = rounded_quotient(root[j], b.s, b.y);
+        y[j] = q > 0.f ? __builtin_amdgcn_fmed3f(q, kLeastCode, kTopCode) : 0.f;
+        if (odd) {                           // (the same for the whole wave)
+            x[j] = fabsf(me[j]) < __builtin_inff() ? x[j] : __builtin_nanf("");
+            y[j] = fabsf(ve[j]) < __builtin_inff() ? y[j] : __builtin_nanf("");
+        }
     }
-    int a = 0, b = 0;
-    a = __builtin_amdgcn_cvt_sr_fp8_f32(m[0] * m_per, words[0], a, 0);
-    b = __builtin_amdgcn_cvt_sr_fp8_f32(x[0], words[0] << 16, b, 0);
-    a = __builtin_amdgcn_cvt_sr_fp8_f32(m[1] * m_per, words[1], a, 1);
-    b = __builtin_amdgcn_cvt_sr_fp8_f32(x[1], words[1] << 16, b, 1);
-    a = __builtin_amdgcn_cvt_sr_fp8_f32(m[2] * m_per, words[2], a, 2);
-    b = __builtin_amdgcn_cvt_sr_fp8_f32(x[2], words[2] << 16, b, 2);
-    a = __builtin_amdgcn_cvt_sr_fp8_f32(m[3] * m_per, words[3], a, 3);
-    b = __builtin_amdgcn_cvt_sr_fp8_f32(x[3], words[3] << 16, b, 3);
-    cm = (uint32_t)a;
-    cr = (uint32_t)b;
+    int p = 0, q = 0;
+    p = __builtin_amdgcn_cvt_sr_fp8_f32(x[0], words[0], p, 0);
+    q = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], words[0] << 16, q, 0);
+    p = __builtin_amdgcn_cvt_sr_fp8_f32(x[1], words[1], p, 1);
+    q = __builtin_amdgcn_cvt_sr_fp8_f32(y[1], words[1] << 16, q, 1);
+    p = __builtin_amdgcn_cvt_sr_fp8_f32(x[2], words[2], p, 2);
+    q = __builtin_amdgcn_cvt_sr_fp8_f32(y[2], words[2] << 16, q, 2);
+    p = __builtin_amdgcn_cvt_sr_fp8_f32(x[3], words[3], p, 3);
+    q = __builtin_amdgcn_cvt_sr_fp8_f32(y[3], words[3] << 16, q, 3);
+    cm = (uint32_t)p;
+    cr = (uint32_t)q;
 }
 __device__ inline uint32_t block_key(const Step& s, int64_t lo) { return s.key ^ (uint32_t)(lo >> 32) * 0x9E3779B1u; }   // a block never crosses 2^32
 
@@ -220,7 +263,10 @@ struct Blocks {
                 numbers_of(v[k], LEGEND_TYPE_FLOAT, ve);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) root[j] = step_element(s, ge[j], me[j], ve[j], pe[j]);
+            for (int j = 0; j < 4; ++j) {
+                if (BLOCK) step_block(s, ge[j], me[j], ve[j], root[j], pe[j]);
+                else step_float(s, ge[j], me[j], ve[j], pe[j]);
+            }
             if (t.master) store_quad<STREAM>(t.master + i, pe);
             put_quad<STREAM>(t.param, i, t.param_type, pe);
             if (!BLOCK) {
@@ -229,13 +275,12 @@ struct Blocks {
                 continue;
             }
             const int64_t at = lo + k * kApart;
-            float m_per, root_per;
-            const float ms = block_scale(me, m_per), vs = block_scale(root, root_per);
             const uint32_t key = block_key(s, at);
             const uint32_t words[4] = {random_word((uint32_t)i ^ key), random_word((uint32_t)(i + 1) ^ key),
                                        random_word((uint32_t)(i + 2) ^ key), random_word((uint32_t)(i + 3) ^ key)};
             uint32_t cm, cr;
-            codes_of(me, m_per, root, root_per, words, cm, cr);
+            float ms, vs;
+            codes_of(me, ve, root, words, cm, cr, ms, vs);
             code_word* to_m = reinterpret_cast<code_word*>(static_cast<uint8_t*>(t.m) + i);
             code_word* to_v = reinterpret_cast<code_word*>(static_cast<uint8_t*>(t.v) + i);
             if (STREAM) {
@@ -257,38 +302,38 @@ struct Blocks {
 __device__ inline void part_block(const AdamTensor& t, const void* grad, const Step& s, int64_t lo) {
     const bool block = t.state_type == LEGEND_STATE_BLOCK;
     const float ms = block ? t.m_scale[lo / kAdamBlock] : 1.f, vs = block ? t.v_scale[lo / kAdamBlock] : 1.f;
-    float m[4], root[4];
+    float m[4], v[4], root[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t i = lo + j * kWave + lane_id();
-        m[j] = root[j] = 0.f;
+        m[j] = v[j] = root[j] = 0.f;
         if (i >= t.count) continue;
-        float v;
         if (block) {
             m[j] = __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(t.m)[i], 0) * ms;
-            v = __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(t.v)[i], 0) * vs;
-            v *= v;
+            v[j] = __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(t.v)[i], 0) * vs;
+            v[j] *= v[j];
         } else {
             m[j] = static_cast<const float*>(t.m)[i];
-            v = static_cast<const float*>(t.v)[i];
+            v[j] = static_cast<const float*>(t.v)[i];
         }
         float p = t.master ? t.master[i] : load_as(t.param, i, t.param_type);
-        root[j] = step_element(s, load_as(grad, i, t.grad_type), m[j], v, p);
+        const float g = load_as(grad, i, t.grad_type);
+        if (block) step_block(s, g, m[j], v[j], root[j], p);
+        else step_float(s, g, m[j], v[j], p);
         if (t.master) t.master[i] = p;
         store_as(t.param, i, t.param_type, p);
         if (!block) {
             static_cast<float*>(t.m)[i] = m[j];
-            static_cast<float*>(t.v)[i] = v;
+            static_cast<float*>(t.v)[i] = v[j];
         }
     }
     if (!block) return;
-    float m_per, root_per;
-    const float new_ms = block_scale(m, m_per), new_vs = block_scale(root, root_per);
     const uint32_t key = block_key(s, lo);
     uint32_t words[4], cm, cr;
+    float new_ms, new_vs;
 #pragma unroll
     for (int j = 0; j < 4; ++j) words[j] = random_word((uint32_t)(lo + j * kWave + lane_id()) ^ key);
-    codes_of(m, m_per, root, root_per, words, cm, cr);
+    codes_of(m, v, root, words, cm, cr, new_ms, new_vs);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t i = lo + j * kWave + lane_id();

@@ -221,26 +221,31 @@ __global__ void __launch_bounds__(1024) k_norm_backward_long(NormParams a) {
     }
 }
 
-// Sums of the workgroups' partial sums, in 64 bits: 32 columns a workgroup, each by 32 threads that take every 32nd part, added
-// in the order of the threads.
+// Sums of the workgroups' partial sums, in 64 bits: 32 columns a workgroup (whole cache lines; with 8, 500 parts of 6000 columns take
+// 10.5 instead of 6.3 us), each by 32 threads that take every 32nd part; added up over the wave, then over the workgroup's waves in
+// order.
 __global__ void __launch_bounds__(1024) k_norm_sums(NormParams a) {
-    __shared__ double box[32][33];
-    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    constexpr int C = 32, SLICES = 1024 / C;
+    __shared__ double box[16][C];
+    const int col = threadIdx.x % C, slice = threadIdx.x / C;
+    const int64_t c = (int64_t)blockIdx.x * C + col;
     const int64_t width = 2 * (int64_t)a.dim;
     double s = 0.0;
     if (c < width) {
 #pragma unroll 8
-        for (int p = slice; p < a.parts; p += 32) s += (double)a.partial[p * width + c];
+        for (int p = slice; p < a.parts; p += SLICES) s += (double)a.partial[p * width + c];
     }
-    box[slice][lane] = s;
+#pragma unroll
+    for (int k = C; k < kWave; k <<= 1) s += __shfl_xor(s, k, kWave);
+    if (lane_id() < C) box[threadIdx.x / kWave][col] = s;
     __syncthreads();
     if (slice || c >= width) return;
     void* out = c < a.dim ? a.dweight : a.dbias;
     if (!out) return;
     const int64_t at = c < a.dim ? c : c - a.dim;
     s = a.accumulate ? (double)load_as(out, at, a.dweight_type) : 0.0;
-    for (int k = 0; k < 32; ++k) s += box[k][lane];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += box[k][col];
     store_as(out, at, a.dweight_type, (float)s);
 }
 

@@ -210,6 +210,15 @@ def test_forward_and_backward(ctx, rows, dim):
     check_backward(case, backward(ctx, case, mean, rstd), case.x64, case.dy64, mean, rstd)
 
 
+@pytest.mark.parametrize("rows,dim", [(700, 5_000), (600, 9_001), (300, 16_384), (600, 20_000), (2_500, 1_028)], ids=lambda v: str(v))
+def test_many_wide_rows(ctx, rows, dim):
+    """Every workgroup takes several rows: what its threads add up from row to row."""
+    case = Case(rows, dim, 1, 1)
+    y, mean, rstd = forward(ctx, case)
+    check_forward(case, y, mean, rstd)
+    check_backward(case, backward(ctx, case, mean, rstd), case.x64, case.dy64, mean, rstd)
+
+
 @pytest.mark.parametrize("wt", [0, 1, 2], ids=["wf", "wb", "wh"])
 @pytest.mark.parametrize("xt,yt", [(0, 0), (0, 1), (0, 2), (1, 1), (1, 0), (2, 2), (2, 0)], ids=["ff", "fb", "fh", "bb", "bf", "hh", "hf"])
 @pytest.mark.parametrize("rows,dim", [(37, 100), (21, 1_001), (9, 2_304), (4, 20_000)], ids=lambda v: str(v))
