@@ -16,7 +16,7 @@ namespace legend {
 constexpr float kTopCode = 448.f;           // largest e4m3 value
 constexpr float kLeastCode = 0.001953125f;  // smallest above zero, 2^-9
 constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100: 1 / scale stays far from infinity
-constexpr float kLeastNormal = 1.17549435e-38f;
+constexpr uint32_t kLeastNormal = 0x00800000u, kInfinity = 0x7f800000u;     // bits of fp32 numbers
 
 // Sets of fewer elements are cut into units of 1024, so that more workgroups share them, and their workgroups all fit the card at a
 // time (five a compute unit by their registers); larger ones into units of 2048, two blocks in flight a wave (four: 344 against 333 us
@@ -28,20 +28,28 @@ constexpr int64_t kGridSmall = 1280, kGridLarge = 2048;      // workgroups of a 
 // read the gradients at 5 TB/s, 1024 at 3.6; 3 M: 24.7 against 25.5 us for the whole step)
 constexpr int kPartsSmall = 1024, kPartsLarge = kAdamNormParts;
 
-// Largest of the wave's numbers, none below zero, in all lanes.  Compared as integers, which orders them alike, with infinity and
-// NaN at the top.
+// Largest of the wave's numbers, of two kinds at a time (data-parallel moves that depend on each other wait), none below zero, in all
+// lanes.  Compared as integers, which orders them alike, with infinity and NaN at the top.
 template <int CTRL>
-__device__ inline uint32_t dpp_word(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false); }
-__device__ inline float wave_max(float top) {
-    uint32_t v = __float_as_uint(top);
-    v = max(v, dpp_word<0xB1>(v));           // lane ^ 1
-    v = max(v, dpp_word<0x4E>(v));           // lane ^ 2
-    v = max(v, dpp_word<0x141>(v));          // mirrored within 8
-    v = max(v, dpp_word<0x140>(v));          // mirrored within 16
-    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    v = max((uint32_t)r[0], (uint32_t)r[1]);
-    const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    return __uint_as_float(max((uint32_t)h[0], (uint32_t)h[1]));
+__device__ inline void max_moved(uint32_t& a, uint32_t& b) {
+    const uint32_t x = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, CTRL, 0xf, 0xf, false);
+    const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, CTRL, 0xf, 0xf, false);
+    a = max(a, x);
+    b = max(b, y);
+}
+__device__ inline void wave_max(uint32_t& a, uint32_t& b) {
+    max_moved<0xB1>(a, b);                   // lane ^ 1
+    max_moved<0x4E>(a, b);                   // lane ^ 2
+    max_moved<0x141>(a, b);                  // mirrored within 8
+    max_moved<0x140>(a, b);                  // mirrored within 16
+    const auto p = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    const auto q = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    a = max((uint32_t)p[0], (uint32_t)p[1]);
+    b = max((uint32_t)q[0], (uint32_t)q[1]);
+    const auto r = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+    const auto t = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    a = max((uint32_t)r[0], (uint32_t)r[1]);
+    b = max((uint32_t)t[0], (uint32_t)t[1]);
 }
 
 // sum of 256 threads' doubles, in every thread
@@ -134,7 +142,7 @@ __device__ inline void step_float(const Step& s, float g, float& m, float& v, fl
 // what it is made from: a root or a quotient that is a bit off is another code once in a million).
 // Root of v: from the hardware's reciprocal root by one step whose residual is exact.  NaN for infinity.
 __device__ inline float rounded_root(float v) {
-    const float c = fmaxf(v, kLeastNormal);
+    const float c = __uint_as_float(max(__float_as_uint(v), kLeastNormal));
     const float y = __builtin_amdgcn_rsqf(c);
     const float q = c * y;
     const float root = fmaf(fmaf(-q, q, c), 0.5f * y, q);
@@ -155,18 +163,22 @@ __device__ inline void step_block(const Step& s, float g, float& m, float& v, fl
     p = step_parameter(s, m, root, p);
 }
 
-// Largest finite magnitude of a wave's numbers, and whether some are not finite.
-__device__ inline float block_top(const float* v, bool& odd) {
-    float top = wave_max(__uint_as_float(max(max(__float_as_uint(fabsf(v[0])), __float_as_uint(fabsf(v[1]))),
-                                             max(__float_as_uint(fabsf(v[2])), __float_as_uint(fabsf(v[3]))))));
-    if (!(top < __builtin_inff())) {
-        odd = true;
-        float t = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) t = fabsf(v[j]) < __builtin_inff() ? fmaxf(t, fabsf(v[j])) : t;
-        top = wave_max(t);
+// Largest finite magnitudes of a wave's first moments and second moments, and whether some are not finite.
+__device__ inline uint32_t bits_of(float v) { return __float_as_uint(fabsf(v)); }
+__device__ inline uint32_t finite_bits(float v) { return bits_of(v) < kInfinity ? bits_of(v) : 0u; }
+__device__ inline bool block_tops(const float* me, const float* ve, float& top_m, float& top_v) {
+    uint32_t a = max(max(bits_of(me[0]), bits_of(me[1])), max(bits_of(me[2]), bits_of(me[3])));
+    uint32_t b = max(max(bits_of(ve[0]), bits_of(ve[1])), max(bits_of(ve[2]), bits_of(ve[3])));
+    wave_max(a, b);
+    const bool odd = max(a, b) >= kInfinity;
+    if (odd) {
+        a = max(max(finite_bits(me[0]), finite_bits(me[1])), max(finite_bits(me[2]), finite_bits(me[3])));
+        b = max(max(finite_bits(ve[0]), finite_bits(ve[1])), max(finite_bits(ve[2]), finite_bits(ve[3])));
+        wave_max(a, b);
     }
-    return top;
+    top_m = __uint_as_float(a);
+    top_v = __uint_as_float(b);
+    return odd;
 }
 struct Scale {
     float s, y;                              // the scale and its reciprocal; both 0 where everything is
@@ -179,8 +191,8 @@ __device__ inline Scale scale_of(float top) {
 // A block's scales and codes from its moments: me and ve, root the roots of ve.  The conversion adds a word's upper 20 bits below the
 // last bit that it keeps.
 __device__ inline void codes_of(const float* me, const float* ve, const float* root, const uint32_t* words, uint32_t& cm, uint32_t& cr, float& ms, float& vs) {
-    bool odd = false;
-    const float top_m = block_top(me, odd), top_v = block_top(ve, odd);
+    float top_m, top_v;
+    const bool odd = block_tops(me, ve, top_m, top_v);
     const Scale a = scale_of(top_m), b = scale_of(rounded_root(top_v));
     ms = a.s;
     vs = b.s;
@@ -190,9 +202,12 @@ __device__ inline void codes_of(const float* me, const float* ve, const float* r
         x[j] = __builtin_amdgcn_fmed3f(rounded_quotient(me[j], a.s, a.y), -kTopCode, kTopCode);
         const float q = rounded_quotient(root[j], b.s, b.y);
         y[j] = q > 0.f ? __builtin_amdgcn_fmed3f(q, kLeastCode, kTopCode) : 0.f;
-        if (odd) {                           // (the same for the whole wave)
-            x[j] = fabsf(me[j]) < __builtin_inff() ? x[j] : __builtin_nanf("");
-            y[j] = fabsf(ve[j]) < __builtin_inff() ? y[j] : __builtin_nanf("");
+    }
+    if (odd) {                               // (the same for the whole wave)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[j] = bits_of(me[j]) < kInfinity ? x[j] : __builtin_nanf("");
+            y[j] = bits_of(ve[j]) < kInfinity ? y[j] : __builtin_nanf("");
         }
     }
     int p = 0, q = 0;
