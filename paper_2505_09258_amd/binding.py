@@ -398,6 +398,10 @@ def legend_unique_rows_read(ctx):
     return u.value, b.value
 
 
+def _address(a) -> Optional[int]:
+    return None if a is None else int(a)
+
+
 def make_layer_norm(*, rows, dim, x=None, x_stride=None, x_type=TYPE_FLOAT, table=-1, ids=None, status=None, weight=None,
                     bias=None, weight_type=TYPE_FLOAT, eps=1e-5, mean=None, rstd=None, y=None, y_stride=None, y_type=None,
                     dy=None, dy_stride=None, dy_type=None, dx=None, dx_stride=None, dweight=None, dbias=None,
@@ -405,10 +409,11 @@ def make_layer_norm(*, rows, dim, x=None, x_stride=None, x_type=TYPE_FLOAT, tabl
     """Arguments of both directions, kept and used again by a program whose buffers stay.  Pointers are device addresses
     (integers; None passes NULL); strides default to dim, y_type and dy_type to x_type."""
     return legend_layer_norm(
-        C.sizeof(legend_layer_norm), dim, rows, x, dim if x_stride is None else x_stride, x_type, table, ids, status, weight, bias,
-        weight_type, eps, mean, rstd, y, dim if y_stride is None else y_stride, x_type if y_type is None else y_type,
-        x_type if dy_type is None else dy_type, dy, dim if dy_stride is None else dy_stride, dx, dim if dx_stride is None else dx_stride,
-        dweight, dbias, dweight_type, int(accumulate), workspace, workspace_bytes)
+        C.sizeof(legend_layer_norm), int(dim), int(rows), _address(x), int(dim if x_stride is None else x_stride), x_type, table, _address(ids),
+        _address(status), _address(weight), _address(bias), weight_type, eps, _address(mean), _address(rstd), _address(y),
+        int(dim if y_stride is None else y_stride), x_type if y_type is None else y_type, x_type if dy_type is None else dy_type, _address(dy),
+        int(dim if dy_stride is None else dy_stride), _address(dx), int(dim if dx_stride is None else dx_stride), _address(dweight),
+        _address(dbias), dweight_type, int(accumulate), _address(workspace), int(workspace_bytes))
 
 
 def legend_layer_norm_forward(ctx, norm: legend_layer_norm) -> None:
@@ -426,7 +431,8 @@ def legend_layer_norm_workspace(rows: int, dim: int) -> int:
 def make_adamw_tensor(*, count, param, grad, m, v, m_scale=None, v_scale=None, master=None, param_type=TYPE_FLOAT,
                       grad_type=TYPE_FLOAT, state_type=STATE_FLOAT, weight_decay=0.0, lr_scale=1.0) -> legend_adamw_tensor:
     """Pointers are device addresses (integers; None passes NULL)."""
-    return legend_adamw_tensor(param, grad, master, m, v, m_scale, v_scale, count, param_type, grad_type, state_type, 0, weight_decay, lr_scale)
+    return legend_adamw_tensor(_address(param), _address(grad), _address(master), _address(m), _address(v), _address(m_scale), _address(v_scale),
+                               int(count), param_type, grad_type, state_type, 0, weight_decay, lr_scale)
 
 
 def legend_adamw_create(ctx, tensors: Sequence[legend_adamw_tensor], *, beta1=0.9, beta2=0.999, eps=1e-8, max_norm=0.0, seed=0):
@@ -442,11 +448,11 @@ def legend_adamw_destroy(opt) -> None:
 
 def legend_adamw_step(opt, lr: float, lr_factor: Optional[int] = None, grad_scale: Optional[int] = None, norm: Optional[int] = None) -> None:
     """lr_factor, grad_scale and norm are device addresses of one float each, or None."""
-    _check(_lib.legend_adamw_step(opt, lr, lr_factor, grad_scale, norm))
+    _check(_lib.legend_adamw_step(opt, lr, _address(lr_factor), _address(grad_scale), _address(norm)))
 
 
 def legend_adamw_set_gradients(opt, grads: Sequence[Optional[int]]) -> None:
-    _check(_lib.legend_adamw_set_gradients(opt, (C.c_void_p * max(len(grads), 1))(*grads), len(grads)))
+    _check(_lib.legend_adamw_set_gradients(opt, (C.c_void_p * max(len(grads), 1))(*map(_address, grads)), len(grads)))
 
 
 def legend_adamw_get_steps(opt):

@@ -27,6 +27,7 @@ struct legend_adamw {
     int64_t units = 0;
     int32_t unit_elems = 0;
     bool stream = false;
+    int32_t kinds = 0;
 };
 
 namespace {
@@ -381,12 +382,14 @@ int legend_adamw_create(legend_ctx* c, const legend_adamw_config* cfg, const leg
     if (!(cfg->max_norm >= 0.0) || !std::isfinite(cfg->max_norm)) return fail(LEGEND_E_INVAL, "max_norm must be finite and not negative");
     std::vector<const void*> grads((size_t)n);
     int64_t total = 0, total_bytes = 0;
+    int32_t kinds = 0;
     for (int64_t k = 0; k < n; ++k) {
         rc = check_tensor(tensors[k], k);
         if (rc) return rc;
         grads[(size_t)k] = tensors[k].grad;
         total += tensors[k].count;
         total_bytes += tensor_bytes(tensors[k]);
+        kinds |= tensors[k].state_type == LEGEND_STATE_BLOCK ? 2 : 1;
         if (total > ((int64_t)1 << 48)) return fail(LEGEND_E_INVAL, "too many elements");
     }
     struct Holder {
@@ -408,6 +411,7 @@ int legend_adamw_create(legend_ctx* c, const legend_adamw_config* cfg, const leg
 
     o->unit_elems = adam_unit_elems(total);
     o->stream = total_bytes > kCacheBytes;
+    o->kinds = kinds;
     std::vector<AdamTensor> desc((size_t)n);
     for (int64_t k = 0; k < n; ++k) {
         const legend_adamw_tensor& t = tensors[k];
@@ -415,7 +419,7 @@ int legend_adamw_create(legend_ctx* c, const legend_adamw_config* cfg, const leg
                                      t.param_type, t.grad_type, t.state_type, (int32_t)k};
         o->units += (t.count + o->unit_elems - 1) / o->unit_elems;
     }
-    if (o->units > 0x7fffffffll) return fail(LEGEND_E_INVAL, "too many elements");
+    if (o->units > (1 << 28)) return fail(LEGEND_E_INVAL, "too many elements");
     std::vector<int32_t> unit_tensor((size_t)o->units);
     for (int64_t k = 0, u = 0; k < n; ++k)
         for (int64_t left = tensors[k].count; left > 0; left -= o->unit_elems) unit_tensor[(size_t)u++] = (int32_t)k;
@@ -496,6 +500,7 @@ int legend_adamw_step(legend_adamw* o, double lr, const float* lr_factor, const 
     a.max_norm = o->cfg.max_norm;
     a.seed = o->cfg.seed;
     a.stream = o->stream ? 1 : 0;
+    a.kinds = o->kinds;
     a.with_norm = o->cfg.max_norm > 0.0 || norm ? 1 : 0;
     DENSE_TRY(o->ctx, launch_adamw(v.stream, a));
     return LEGEND_OK;

@@ -224,10 +224,15 @@ __device__ inline void codes_of(const float* me, const float* ve, const float* r
 }
 __device__ inline uint32_t block_key(const Step& s, int64_t lo) { return s.key ^ (uint32_t)(lo >> 32) * 0x9E3779B1u; }   // a block never crosses 2^32
 
+// Which states the tensors of a call have: one kind alone takes fewer registers.
+enum StateKinds { FLOAT_STATES = 1, BLOCK_STATES = 2, BOTH_STATES = 3 };
+template <int KINDS>
+__device__ inline bool has_blocks(const AdamTensor& t) { return KINDS == BLOCK_STATES || (KINDS == BOTH_STATES && t.state_type == LEGEND_STATE_BLOCK); }
+
 // K whole blocks of 256 elements as a wave loads them, kApart elements from one to the next: four neighbouring elements a lane.
 constexpr int kApart = 4 * kAdamBlock;
 typedef uint32_t code_word __attribute__((aligned(1)));
-template <int K, bool STREAM>
+template <int K, bool STREAM, int KINDS>
 struct Blocks {
     uint4 g[K], p[K], m[K], v[K];            // 8-bit states: four codes in m.x and v.x, the block's scales in m.y and v.y
 
@@ -240,7 +245,7 @@ struct Blocks {
             g[k] = raw_quad<false>(grad, i0 + k * kApart, t.grad_type);
             p[k] = raw_quad<STREAM>(from, i0 + k * kApart, ptype);
         }
-        if (t.state_type == LEGEND_STATE_BLOCK) {
+        if (has_blocks<KINDS>(t)) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const code_word* cm = reinterpret_cast<const code_word*>(static_cast<const uint8_t*>(t.m) + i0 + k * kApart);
@@ -314,8 +319,9 @@ struct Blocks {
 };
 
 // The last block of a tensor, elements [lo, count): single elements, neighbours in neighbouring lanes.
+template <int KINDS>
 __device__ inline void part_block(const AdamTensor& t, const void* grad, const Step& s, int64_t lo) {
-    const bool block = t.state_type == LEGEND_STATE_BLOCK;
+    const bool block = has_blocks<KINDS>(t);
     const float ms = block ? t.m_scale[lo / kAdamBlock] : 1.f, vs = block ? t.v_scale[lo / kAdamBlock] : 1.f;
     float m[4], v[4], root[4];
 #pragma unroll
@@ -413,7 +419,7 @@ __global__ void __launch_bounds__(256) k_grad_squares(AdamParams a) {
     if (threadIdx.x == 0) a.partial[blockIdx.x] = all;
 }
 
-template <int K, bool STREAM>
+template <int K, bool STREAM, int KINDS>
 __global__ void __launch_bounds__(256) k_adamw(AdamParams a, int norm_parts) {
     __shared__ double box[4];
     const TensorTable tensors = (TensorTable)a.tensors;
@@ -450,7 +456,7 @@ __global__ void __launch_bounds__(256) k_adamw(AdamParams a, int norm_parts) {
         const void* grad = grads[k0];
         const int64_t unit_lo = (u - t.first_unit) * (K * kApart), lo = unit_lo + (threadIdx.x / kWave) * kAdamBlock;
         const bool whole = unit_lo + K * kApart <= t.count;
-        Blocks<K, STREAM> in;
+        Blocks<K, STREAM, KINDS> in;
         if (whole) in.load(t, grad, lo);
         if (!ready) prepare();                   // the first unit's numbers are on their way meanwhile
         if (skip) break;
@@ -459,18 +465,18 @@ __global__ void __launch_bounds__(256) k_adamw(AdamParams a, int norm_parts) {
         s.keep = (float)(1.0 - tlr * t.weight_decay);
         s.key = (uint32_t)hash_fold(key, (uint64_t)t.index);
         if (whole) {
-            if (t.state_type == LEGEND_STATE_BLOCK) in.template finish<true>(t, s, lo);
+            if (has_blocks<KINDS>(t)) in.template finish<true>(t, s, lo);
             else in.template finish<false>(t, s, lo);
         } else {
             for (int k = 0; k < K; ++k) {
                 const int64_t at = lo + k * kApart;
                 if (at >= t.count) break;
                 if (at + kAdamBlock > t.count) {
-                    part_block(t, grad, s, at);
+                    part_block<KINDS>(t, grad, s, at);
                 } else {
-                    Blocks<1, STREAM> one;
+                    Blocks<1, STREAM, KINDS> one;
                     one.load(t, grad, at);
-                    if (t.state_type == LEGEND_STATE_BLOCK) one.template finish<true>(t, s, at);
+                    if (has_blocks<KINDS>(t)) one.template finish<true>(t, s, at);
                     else one.template finish<false>(t, s, at);
                 }
             }
@@ -505,7 +511,9 @@ static hipError_t launch_units(hipStream_t st, const AdamParams& a) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t grid = a.units < 1 ? 1 : (a.units < most ? a.units : most);
-    k_adamw<K, STREAM><<<(unsigned)grid, 256, 0, st>>>(a, parts);
+    if (a.kinds == FLOAT_STATES) k_adamw<K, STREAM, FLOAT_STATES><<<(unsigned)grid, 256, 0, st>>>(a, parts);
+    else if (a.kinds == BLOCK_STATES) k_adamw<K, STREAM, BLOCK_STATES><<<(unsigned)grid, 256, 0, st>>>(a, parts);
+    else k_adamw<K, STREAM, BOTH_STATES><<<(unsigned)grid, 256, 0, st>>>(a, parts);
     return hipGetLastError();
 }
 

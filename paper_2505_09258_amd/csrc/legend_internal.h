@@ -258,6 +258,7 @@ struct AdamParams {
     double lr, beta1, beta2, eps, max_norm;
     uint64_t seed;
     int32_t with_norm;
+    int32_t kinds;                          // 1: tensors with 32-bit states, 2: with 8-bit ones, 3: both
     int32_t stream;                         // parameters and states are marked as streaming
 };
 int adam_unit_elems(int64_t total);
