@@ -1,8 +1,8 @@
 // AdamW over many tensors in one launch, with the norm of all gradients in a launch before it where it is asked for.
 //
-// Every tensor is cut into units of unit_elems elements, the last one partial; a workgroup takes units in turn, so that
-// hundreds of small tensors and a few large ones fill the card alike.  Nothing is exchanged between workgroups: each adds up the
-// partial sums of the norm by itself (8 KB from L2), in one order, in 64 bits.
+// Every tensor is cut into units of unit_elems elements, the last one partial, so that hundreds of small tensors and a few large
+// ones fill the card alike.  Nothing is exchanged between the workgroups of a kernel.  The norm's sums are taken in 64 bits and in one
+// order.
 //
 // 8-bit states: a wave owns a block of 256 elements; its largest |m| and sqrt(v) set the block's scales.
 #include "legend_internal.h"
@@ -19,13 +19,14 @@ constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100: 1 / scale stays far fr
 constexpr uint32_t kLeastNormal = 0x00800000u, kInfinity = 0x7f800000u;     // bits of fp32 numbers
 
 // Sets of fewer elements are cut into units of 1024, so that more workgroups share them, and their workgroups all fit the card at a
-// time (five a compute unit by their registers); larger ones into units of 2048, two blocks in flight a wave (four: 344 against 333 us
-// for 60 M fp32 parameters, 515 against 417 for 120 M bf16 with 8-bit states: too many registers; units of 2048 for 3 M elements: 28.0
-// against 24.8).
+// time; each adds up the norm's partial sums by itself, which is less than a launch takes.  Larger sets are cut into units of 2048, two
+// blocks in flight a wave (four: 515 against 417 us for 120 M bf16 parameters with 8-bit states, too many registers; units of 2048 for
+// 3 M elements: 28.0 against 24.8), one unit a workgroup (1024 workgroups that take units in turn: 358 against 335 us), and a kernel
+// of one workgroup adds the partial sums up.
 constexpr int64_t kLargeTotal = 4 << 20;
-constexpr int64_t kGridSmall = 1280, kGridLarge = 2048;      // workgroups of a step
-// of the kernel of the squares, each with a partial sum that every workgroup of a step adds up again (120 M elements: 2048 of them
-// read the gradients at 5 TB/s, 1024 at 3.6; 3 M: 24.7 against 25.5 us for the whole step)
+constexpr int64_t kGridSmall = 1280;
+// Workgroups of the kernel of the squares.  (120 M elements: 2048 of them read the gradients at 5 TB/s, 1024 at 3.6; 3 M: 24.7 against
+// 25.5 us for the whole step)
 constexpr int kPartsSmall = 1024, kPartsLarge = kAdamNormParts;
 
 // Largest of the wave's numbers, of two kinds at a time (data-parallel moves that depend on each other wait), none below zero, in all
@@ -368,8 +369,8 @@ __device__ inline void part_block(const AdamTensor& t, const void* grad, const S
     }
 }
 
-// What a step reads of the state and what it leaves lie apart: its first kernel (this one's first thread, in the kernel of the
-// squares, or alone) makes the one from the other, its last writes the other.  No workgroup waits for another, and a counter of
+// What a step reads of the state and what it leaves lie apart: a kernel before its last one (the squares', the one that finishes the
+// norm, or one for this alone) makes the one from the other, its last writes the other.  No workgroup waits for another, and a counter of
 // finished workgroups, which would tell the last one, costs 10 ns for each of them.
 __device__ inline void begin_step(const AdamParams& a) {
     AdamState& st = *a.state;
@@ -383,12 +384,35 @@ __device__ inline void begin_step(const AdamParams& a) {
 }
 __global__ void k_begin_step(AdamParams a) { begin_step(a); }
 
+// What the gradients are multiplied by, from the partial sums; the same in every thread of 256.
+__device__ inline float gradient_scale(const AdamParams& a, int parts, double* box, bool reports, bool& skip) {
+    float scale = a.grad_scale ? *a.grad_scale : 1.f;
+    skip = false;
+    if (!a.with_norm) return scale;
+    double sum = 0.0;
+    for (int k = threadIdx.x; k < parts; k += 256) sum += a.partial[k];
+    const double norm = sqrt(block_sum(sum, box)) * fabs((double)scale);
+    skip = !(norm < __builtin_inf());
+    if (a.norm_out && reports) *a.norm_out = (float)norm;
+    if (a.max_norm > 0.0 && norm > a.max_norm) scale = (float)(a.max_norm / (norm + 1e-6)) * scale;
+    return scale;
+}
+__global__ void __launch_bounds__(256) k_finish_norm(AdamParams a, int parts) {
+    __shared__ double box[4];
+    bool skip;
+    const float scale = gradient_scale(a, parts, box, threadIdx.x == 0, skip);
+    if (threadIdx.x) return;
+    begin_step(a);
+    a.state->scale = scale;
+    a.state->skip = skip ? 1u : 0u;
+}
+
 // K: blocks that a wave takes of a unit (unit_elems = 4 K blocks).
 template <int K>
 __global__ void __launch_bounds__(256) k_grad_squares(AdamParams a) {
     __shared__ double box[4];
     double s[4] = {0.0, 0.0, 0.0, 0.0};
-    if (blockIdx.x == 0 && threadIdx.x == 0) begin_step(a);
+    if (K == 1 && blockIdx.x == 0 && threadIdx.x == 0) begin_step(a);
     const TensorTable tensors = (TensorTable)a.tensors;
     const UnitTable units = (UnitTable)a.unit_tensor;
     const GradTable grads = (GradTable)a.grads;
@@ -434,14 +458,11 @@ __global__ void __launch_bounds__(256) k_adamw(AdamParams a, int norm_parts) {
         inv_bias1 = a.state->inv_bias1;
         key = a.state->key;
         s.inv_bias2_root = a.state->inv_bias2_root;
-        s.scale = a.grad_scale ? *a.grad_scale : 1.f;
-        if (a.with_norm) {
-            double sum = 0.0;
-            for (int k = threadIdx.x; k < norm_parts; k += 256) sum += a.partial[k];
-            const double norm = sqrt(block_sum(sum, box)) * fabs((double)s.scale);
-            skip = !(norm < __builtin_inf());
-            if (a.norm_out && blockIdx.x == 0 && threadIdx.x == 0) *a.norm_out = (float)norm;
-            if (a.max_norm > 0.0 && norm > a.max_norm) s.scale = (float)(a.max_norm / (norm + 1e-6)) * s.scale;
+        if (K > 1) {
+            s.scale = a.state->scale;
+            skip = a.state->skip != 0;
+        } else {
+            s.scale = gradient_scale(a, norm_parts, box, blockIdx.x == 0 && threadIdx.x == 0, skip);
         }
         lr = a.lr * (a.lr_factor ? (double)*a.lr_factor : 1.0);
         s.b1 = (float)a.beta1;
@@ -504,13 +525,15 @@ void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2) {
 
 template <int K, bool STREAM>
 static hipError_t launch_units(hipStream_t st, const AdamParams& a) {
-    const int64_t most_parts = K > 1 ? kPartsLarge : kPartsSmall, most = K > 1 ? kGridLarge : kGridSmall;
+    const int64_t most_parts = K > 1 ? kPartsLarge : kPartsSmall;
     const int parts = (int)(a.units < most_parts ? a.units : most_parts);
-    if (a.with_norm && parts > 0) k_grad_squares<K><<<parts, 256, 0, st>>>(a);
-    else k_begin_step<<<1, 1, 0, st>>>(a);
+    const bool squares = a.with_norm && parts > 0;
+    if (squares) k_grad_squares<K><<<parts, 256, 0, st>>>(a);
+    if (K > 1) k_finish_norm<<<1, 256, 0, st>>>(a, parts);
+    else if (!squares) k_begin_step<<<1, 1, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t grid = a.units < 1 ? 1 : (a.units < most ? a.units : most);
+    const int64_t grid = a.units < 1 ? 1 : (K > 1 || a.units < kGridSmall ? a.units : kGridSmall);
     if (a.kinds == FLOAT_STATES) k_adamw<K, STREAM, FLOAT_STATES><<<(unsigned)grid, 256, 0, st>>>(a, parts);
     else if (a.kinds == BLOCK_STATES) k_adamw<K, STREAM, BLOCK_STATES><<<(unsigned)grid, 256, 0, st>>>(a, parts);
     else k_adamw<K, STREAM, BOTH_STATES><<<(unsigned)grid, 256, 0, st>>>(a, parts);

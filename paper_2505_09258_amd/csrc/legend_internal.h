@@ -245,6 +245,8 @@ struct AdamState {                          // device; what the next step needs 
     uint64_t key;                           // fold(seed, t)
     int64_t now_steps, now_skipped;
     double now_power1, now_power2;
+    float scale;                            // of the gradients, and whether the step is skipped: where a kernel
+    uint32_t skip;                          // between the two finds them for all workgroups
 };
 struct AdamParams {
     const AdamTensor* tensors;
