@@ -395,6 +395,9 @@ enum { LEGEND_TYPE_FLOAT = 0, LEGEND_TYPE_BFLOAT = 1, LEGEND_TYPE_HALF = 2 };
  * bits, so that one look at *status covers many calls.  A table's call recorded into a graph reads the partitions where
  * they were when it was recorded: record it again after a swap.
  *
+ * A number that is not finite makes its row's y, mean, rstd and dx, and dweight, NaN; numbers beyond 1e18, whose squares leave fp32,
+ * make their row's results meaningless, no other row's.
+ *
  * One struct serves both directions: legend_layer_norm_forward reads the first three groups and writes the last line of the
  * third and the fourth; legend_layer_norm_backward reads mean and rstd as the forward pass wrote them, and the fifth.
  * Memory: outputs must not overlap anything else the call uses, except that y may be x itself, and dx may be x or dy itself
@@ -453,12 +456,13 @@ int64_t legend_layer_norm_workspace(int64_t rows, int32_t dim);
  * With max_norm > 0 or a norm output asked for, a step whose norm is not finite changes nothing and counts as skipped.
  * Without both the norm is not computed and such gradients go through the formulas.  The root of a v below 2^-126
  * counts as some number below 2^-62; with 8-bit states, a v beyond fp32 makes its element NaN.
- * The number of steps lives on the device, so that a recorded step replays as the next one.
+ * The number of steps lives on the device, so that a recorded step replays as the next one.  Steps of one optimiser must not overlap in
+ * time (a graph replayed on another stream than the context's is ordered by the caller).
  *
  * States: LEGEND_STATE_FLOAT: m, v [count] fp32.  LEGEND_STATE_BLOCK: 8 bits; m and v hold m and sqrt(v) as e4m3 codes (1 sign, 4
  * exponent, 3 mantissa bits, largest 448; 0x7f and 0xff: NaN) in units of an fp32 scale for each block of 256 consecutive
- * elements, scale = max |.| / 448 over the block's finite values (below 2^-100: 0, and the block's codes too).  The update of p uses the
- * unrounded m and v.  A value x in units of the scale is rounded stochastically: up from the code below it with the
+ * elements, scale = max |.| * (1 / 448) over the block's finite values (below 2^-100: 0, and the block's codes too).  The update of p
+ * uses the unrounded m and v.  Up to the code every operation is fp32, rounded to nearest, in the order written here.  A value x in units of the scale is rounded stochastically: up from the code below it with the
  * probability of its fraction, so that moments which change by less than a code's step (beta2 = 0.999 changes sqrt(v) by
  * 0.05 % a step, codes are 6 to 12 % apart) still follow on average.  The random word w of element e of tensor k at step t is a
  * counter hash, w = mix(low32(e) ^ low32(e / 2^32) * 0x9E3779B1 ^ low32(fold(fold(seed, t), k))) with fold as in
@@ -505,8 +509,8 @@ int legend_adamw_create(legend_ctx* ctx, const legend_adamw_config* cfg, const l
 /* Waits for the optimiser's work and frees it.  It may come after legend_destroy of its context (every other call is then
  * refused with LEGEND_E_STATE).  NULL is accepted. */
 int legend_adamw_destroy(legend_adamw* opt);
-/* One step.  lr >= 0; lr_factor and grad_scale: one fp32 each on the device, read when the step runs, or NULL for 1;
- * norm: one fp32 on the device, or NULL. */
+/* One step.  lr >= 0; lr_factor and grad_scale (>= 0): one fp32 each on the device, read when the step runs, or NULL for 1;
+ * norm: one fp32 on the device, or NULL.  None of them may lie in the tensors, states or gradients, nor norm be one of the others. */
 int legend_adamw_step(legend_adamw* opt, double lr, const float* lr_factor, const float* grad_scale, float* norm);
 /* Other gradient buffers for the same tensors, in their order (types as at creation).  Waits for the compute stream; not
  * while it is recording. */

@@ -4,7 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstring>
+#include <utility>
 #include <vector>
 
 #include "host_guard.h"
@@ -28,6 +28,7 @@ struct legend_adamw {
     int32_t unit_elems = 0;
     bool stream = false;
     int32_t kinds = 0;
+    std::vector<std::pair<uintptr_t, uintptr_t>> used;      // memory of tensors, states and gradients: disjoint, in order
 };
 
 namespace {
@@ -162,7 +163,8 @@ int enter_opt(legend_adamw* o, CtxView* v) {
 }
 
 // Memory that a step writes overlaps nothing else that it uses; read-only gradients may share memory.
-int check_apart(const std::vector<legend_adamw_tensor>& ts, const void* const* grads) {
+// `used` receives all of it.
+int check_apart(const std::vector<legend_adamw_tensor>& ts, const void* const* grads, std::vector<std::pair<uintptr_t, uintptr_t>>* used) {
     struct Piece {
         uintptr_t lo, hi;
         bool written;
@@ -193,7 +195,19 @@ int check_apart(const std::vector<legend_adamw_tensor>& ts, const void* const* g
         if (p.written) end_written = std::max(end_written, p.hi);
         end_any = std::max(end_any, p.hi);
     }
+    used->clear();
+    for (const Piece& p : all) {
+        if (!used->empty() && p.lo <= used->back().second) used->back().second = std::max(used->back().second, p.hi);
+        else used->push_back({p.lo, p.hi});
+    }
     return LEGEND_OK;
+}
+
+// whether one fp32 at p lies in the optimiser's memory
+bool lies_in(const std::vector<std::pair<uintptr_t, uintptr_t>>& used, const float* p) {
+    if (!p) return false;
+    auto it = std::upper_bound(used.begin(), used.end(), (uintptr_t)p + 3, [](uintptr_t x, const std::pair<uintptr_t, uintptr_t>& r) { return x < r.first; });
+    return it != used.begin() && (uintptr_t)p < (--it)->second;
 }
 
 int check_tensor(const legend_adamw_tensor& t, int64_t k) {
@@ -404,7 +418,7 @@ int legend_adamw_create(legend_ctx* c, const legend_adamw_config* cfg, const leg
     o->device = v.device;
     o->cfg = *cfg;
     o->tensors.assign(tensors, tensors + n);
-    rc = check_apart(o->tensors, grads.data());
+    rc = check_apart(o->tensors, grads.data(), &o->used);
     if (rc) return rc;
     rc = refuse_recording(c, v.stream, "an optimiser cannot be created");
     if (rc) return rc;
@@ -482,6 +496,8 @@ int legend_adamw_step(legend_adamw* o, double lr, const float* lr_factor, const 
     if (rc) return rc;
     if (!(lr >= 0.0) || !std::isfinite(lr)) return fail(LEGEND_E_INVAL, "lr must be finite and not negative");
     if (!aligned_to(lr_factor, 4) || !aligned_to(grad_scale, 4) || !aligned_to(norm, 4)) return fail(LEGEND_E_INVAL, "a scalar is not aligned to its type");
+    if (lies_in(o->used, lr_factor) || lies_in(o->used, grad_scale) || lies_in(o->used, norm) || (norm && (norm == lr_factor || norm == grad_scale)))
+        return fail(LEGEND_E_INVAL, "lr_factor, grad_scale or norm lies in other memory of the step");
     AdamParams a{};
     a.tensors = o->d_tensors;
     a.grads = o->d_grads;
@@ -520,12 +536,14 @@ int legend_adamw_set_gradients(legend_adamw* o, const void* const* grads, int64_
         if (t.count > 0 && (!grads[k] || !aligned_to(grads[k], type_size(t.grad_type))))
             return fail(LEGEND_E_INVAL, "gradient %lld is NULL or not aligned to its elements", (long long)k);
     }
-    rc = check_apart(o->tensors, grads);
+    std::vector<std::pair<uintptr_t, uintptr_t>> used;
+    rc = check_apart(o->tensors, grads, &used);
     if (rc) return rc;
     rc = refuse_recording(o->ctx, v.stream, "gradients cannot be set");
     if (rc) return rc;
     DENSE_TRY(o->ctx, hipMemcpyAsync(o->d_grads, grads, sizeof(void*) * (size_t)n, hipMemcpyHostToDevice, v.stream));
     DENSE_TRY(o->ctx, hipStreamSynchronize(v.stream));
+    o->used.swap(used);
     return LEGEND_OK;
     });
 }

@@ -259,6 +259,22 @@ def test_adamw_refuses_steps_and_gradients(lib, ctx):
     assert lib.legend_adamw_destroy(opt) == OK and lib.legend_adamw_destroy(None) == OK
 
 
+def test_adamw_refuses_scalars_in_its_memory(lib, ctx):
+    rc, opt = create(lib, ctx, [tensor(0), block(1)])
+    assert rc == OK
+    last = at(0) + 4 * 999                                            # of the first tensor's parameter
+    for k in (0, 1, 2):
+        for p in (at(0), last, at(1) + 8, at(12) + 996, at(14), at(15) + 12):
+            assert lib.legend_adamw_step(opt, 1e-3, *[p if j == k else None for j in range(3)]) == INVAL
+        for p in (last + 4, at(12) + 1_000, at(14) + 16, at(0) - 4):
+            assert lib.legend_adamw_step(opt, 1e-3, *[p if j == k else None for j in range(3)]) == OK
+    assert lib.legend_adamw_step(opt, 1e-3, at(60), None, at(60)) == lib.legend_adamw_step(opt, 1e-3, None, at(60), at(60)) == INVAL
+    assert lib.legend_adamw_step(opt, 1e-3, at(60), at(60), at(61)) == OK
+    assert lib.legend_adamw_set_gradients(opt, (C.c_void_p * 2)(at(62), at(63)), 2) == OK
+    assert lib.legend_adamw_step(opt, 1e-3, None, None, at(62)) == INVAL and lib.legend_adamw_step(opt, 1e-3, None, None, at(1)) == OK
+    assert lib.legend_adamw_destroy(opt) == OK
+
+
 def test_adamw_while_recording(lib, ctx):
     rc, opt = create(lib, ctx, [tensor()])
     lib.stub_set(ctx, 1, 0, 0)

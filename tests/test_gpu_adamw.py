@@ -129,7 +129,7 @@ def check_codes(codes, scales, x, word_share, least, err):
     assert len(x) < 300 or sure.mean() > 0.95
 
 
-def check_step(t, before, t_now, k, scale, lr, seed, hyper=HYPER):
+def check_step(t, before, t_now, k, scale, lr, seed, hyper=HYPER, first=0):
     """Tensor t after step t_now, from its numbers before; scale = grad_scale * clip in 64 bits."""
     lr = lr * t.lr_scale
     g = before["g"] * scale
@@ -152,7 +152,7 @@ def check_step(t, before, t_now, k, scale, lr, seed, hyper=HYPER):
         import torch
         assert torch.equal(t.param[1], t.master[1].to(t.param[1].dtype))
     if t.block:
-        w = od.random_words(seed, t_now, k, t.count)
+        w = od.random_words(seed, t_now, k, t.count, first)
         check_codes(after["cm"], after["sm"], m, (w >> np.uint64(12)) / 2.0**20, False, 7 * E * m_terms)
         check_codes(after["cr"], after["sr"], np.sqrt(v), (w & np.uint64(0xFFFF)) / 2.0**16, True, 8 * E * np.sqrt(v))
     assert all(guards_kept(x) for x in t.parts())
@@ -217,6 +217,40 @@ def test_many_tensors_of_all_kinds(ctx, max_norm):
 def test_many_units(ctx, block):
     """More units than workgroups, the last ones partial."""
     run_steps(ctx, [Tensor(3_000_017, block=block), Tensor(5, block=block), Tensor(9_000_001, 1, 1, block, True, shift=1)], steps=1, max_norm=1.0)
+
+
+@pytest.mark.parametrize("block", [False, True], ids=["float", "block"])
+def test_a_tensor_of_more_than_two_to_the_32_elements(ctx, block):
+    """Zeros but for 4096 elements around element 2^32 and at the end, which are compared; everything else stays zero."""
+    import torch
+    from paper_2505_09258_amd import binding as L
+    n, seed = 2**32 + 3_000, 21
+    spans = [(2**32 - 2_048, 2**32 + 2_048), (n - 600, n)]
+    pieces = [Tensor(b - a, 1, 1, block, seed=k) for k, (a, b) in enumerate(spans)]
+    # the spans begin on a block, so that the pieces' scales are the tensor's
+    spans[1] = (n - n % 256, n)
+    pieces[1] = Tensor(n % 256, 1, 1, block, seed=1)
+    big = {k: torch.zeros(n, dtype=t, device="cuda") for k, t in (("param", torch.bfloat16), ("grad", torch.bfloat16), ("m", torch.uint8 if block else torch.float32),
+                                                                  ("v", torch.uint8 if block else torch.float32))}
+    if block:
+        big.update(m_scale=torch.zeros(-(-n // 256), device="cuda"), v_scale=torch.zeros(-(-n // 256), device="cuda"))
+    for p, (a, b) in zip(pieces, spans):
+        for k, t in big.items():
+            lo, hi = (a // 256, -(-b // 256)) if k.endswith("scale") else (a, b)
+            t[lo:hi] = getattr(p, k)[1]
+    opt = L.legend_adamw_create(ctx, [L.make_adamw_tensor(count=n, param_type=1, grad_type=1, state_type=int(block), weight_decay=0.01, **{k: t.data_ptr() for k, t in big.items()})],
+                                seed=seed, max_norm=1e6, **HYPER)
+    torch.cuda.synchronize()
+    L.legend_adamw_step(opt, 0.01)
+    L.legend_adamw_destroy(opt)
+    for p, (a, b) in zip(pieces, spans):
+        before = p.numbers()
+        for k, t in big.items():
+            lo, hi = (a // 256, -(-b // 256)) if k.endswith("scale") else (a, b)
+            getattr(p, k)[1].copy_(t[lo:hi])
+        check_step(p, before, 1, 0, 1.0, 0.01, seed, first=a)
+    assert not bool(big["param"][: spans[0][0]].any()) and not bool(big["param"][spans[0][1]:spans[1][0]].any())
+    assert not bool(big["v"][: spans[0][0]].any()) and not bool(big["v"][spans[0][1]:spans[1][0]].any())
 
 
 @pytest.mark.parametrize("hyper", [dict(beta1=0.0, beta2=0.0, eps=1e-3), dict(beta1=0.5, beta2=0.9, eps=1e-6)], ids=["none", "short"])

@@ -340,6 +340,31 @@ def test_the_same_bits_again(ctx, rows, dim):
     assert bool((y == y2).all()) and all(bool((a[k] == b[k]).all()) for k in a)
 
 
+def test_rows_more_than_two_to_the_32_elements_apart(ctx):
+    """Three rows of half precision, 2^31 + 8 elements from one to the next; what lies between them is never touched."""
+    import torch
+    from paper_2505_09258_amd import binding as L
+    dim, stride = 333, 2**31 + 8
+    case = Case(3, dim, 2, 2)
+    far = [torch.empty(2 * stride + dim + 8, dtype=torch.float16, device="cuda") for _ in range(4)]
+    row = lambda t: torch.as_strided(t, (3, dim), (stride, 1))  # noqa: E731
+    x, dy, y, dx = (row(t) for t in far)
+    x.copy_(case.x[1][:, :dim])
+    dy.copy_(case.dy[1][:, :dim])
+    mean, rstd = torch.empty(3, device="cuda"), torch.empty(3, device="cuda")
+    dw, db = torch.empty(dim, device="cuda"), torch.empty(dim, device="cuda")
+    size = L.legend_layer_norm_workspace(3, dim)
+    space = torch.empty(size // 4, device="cuda")
+    args = case.args(x=x.data_ptr(), x_stride=stride, y=y.data_ptr(), y_stride=stride, dy=dy.data_ptr(), dy_stride=stride, dy_type=2, dx=dx.data_ptr(), dx_stride=stride,
+                     mean=mean.data_ptr(), rstd=rstd.data_ptr(), dweight=dw.data_ptr(), dbias=db.data_ptr(), workspace=space.data_ptr(), workspace_bytes=size)
+    torch.cuda.synchronize()
+    L.legend_layer_norm_forward(ctx, args)
+    L.legend_layer_norm_backward(ctx, args)
+    L.legend_sync(ctx)
+    check_forward(case, y, mean, rstd)
+    check_backward(case, dict(dx=dx, dweight=dw, dbias=db), case.x64, case.dy64, mean, rstd)
+
+
 # ---- rows of the tables -----------------------------------------------------------------------------------------------
 
 
