@@ -231,10 +231,10 @@ int check_tensor(const legend_adamw_tensor& t, int64_t k) {
     return LEGEND_OK;
 }
 
-// Where parameters, states and gradients of all tensors do not fit the Infinity Cache together, a step marks the first two as
-// streaming, so that the gradients, which the norm has just read, are still there for it.  (60 M fp32 parameters, 1.7 GB: 355 against
-// 401 us; 5 M, 140 MB, where everything stays in the cache from step to step: 44 against 39.)
-constexpr int64_t kCacheBytes = (int64_t)256 << 20;
+// Where parameters, states and gradients of all tensors take more than half of the Infinity Cache, a step marks the first two as
+// streaming, so that the gradients, which the norm has just read, are still there for it.  (fp32, marked against not: 100 MB 37 and 33 us, where
+// everything stays in the cache from step to step; 160 MB 52 and 56, 240 MB 72 and 81, 1.2 GB 312 and 374.)
+constexpr int64_t kStreamBytes = (int64_t)128 << 20;
 int64_t tensor_bytes(const legend_adamw_tensor& t) {
     return t.count * (type_size(t.param_type) + type_size(t.grad_type) + (t.master ? 4 : 0) + (t.state_type == LEGEND_STATE_BLOCK ? 2 : 8));
 }
@@ -424,7 +424,7 @@ int legend_adamw_create(legend_ctx* c, const legend_adamw_config* cfg, const leg
     if (rc) return rc;
 
     o->unit_elems = adam_unit_elems(total);
-    o->stream = total_bytes > kCacheBytes;
+    o->stream = total_bytes > kStreamBytes;
     o->kinds = kinds;
     std::vector<AdamTensor> desc((size_t)n);
     for (int64_t k = 0; k < n; ++k) {

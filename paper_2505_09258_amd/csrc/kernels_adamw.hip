@@ -4,7 +4,12 @@
 // ones fill the card alike.  Nothing is exchanged between the workgroups of a kernel.  The norm's sums are taken in 64 bits and in one
 // order.
 //
-// 8-bit states: a wave owns a block of 256 elements; its largest |m| and sqrt(v) set the block's scales.
+// 8-bit states: a wave owns a block of 256 elements, four neighbouring ones a lane; its largest |m| and v set the block's scales.
+//
+// Bound by HBM: 60 M fp32 parameters in 310 us, 5.4 TB/s of what a step cannot do without (first form, one element a thread: 687; with a
+// counter of finished workgroups at the end, 10 ns a workgroup: 20 us more); 120 M bf16 parameters with master copies and 8-bit states in
+// 357 us, 5.4 TB/s (1476; with divisions and roots as the compiler expands them 490).  The gradients are read twice, the second time from
+// the cache where they fit.  Small sets are bound by their launches: 41 000 elements in 8 us.
 #include "legend_internal.h"
 #include "device_utils.h"
 #include "tensor_types.h"

@@ -7,8 +7,10 @@
 // What the rounding of the mean to fp32 leaves, left = sum c / d, is taken off in the same sweep: var = sum c^2 / d - left^2,
 // and by a third sum where left^2 is more than kLeftShare of the first term (rows whose spread is lost in their offset).
 //
-// A row stays in the registers of 8 to 1024 threads from its one read to its one write; weight and bias stay there from row
-// to row.  Bound by HBM: an element is read and written once, for some ten vector instructions.
+// A row stays in the registers of 8 to 512 threads from its one read to its one write; weight and bias stay there from row to row,
+// and the next row's loads are on their way while a row is worked on.  Bound by HBM: an element is read and written once, for some
+// ten vector instructions.  16384 x 4096 bf16: 51 us, 5.3 TB/s (a workgroup a row that reads it again for every sweep: 267 us; without the
+// loads ahead and with a branch at each of them: 86); 50 000 x 100 table rows to bf16: 10.3 us, of which 2.5 are a launch's.
 #include "norm_rows.h"
 
 #include <type_traits>
@@ -182,7 +184,8 @@ hipError_t launch_norm_forward(hipStream_t st, const NormParams& a) {
         } else {
             for_shape<1, 256>(a.dim, [&](auto s) {
                 typedef decltype(s) S;
-                // at most the 2048 threads that a compute unit holds, so that weight and bias are loaded once a workgroup
+                // at most the 2048 threads that a compute unit holds, so that weight and bias are loaded once a workgroup (one row a
+                // workgroup: 63 against 51 us for 16384 x 4096 bf16)
                 const int64_t need = (a.rows + S::groups * S::R - 1) / (S::groups * S::R), most = 256 * 2048 / S::threads;
                 const unsigned grid = (unsigned)(need < most ? need : most);
                 if (!a.status) k_norm_forward<XT, YT, S, false><<<grid, S::threads, 0, st>>>(a);
