@@ -17,7 +17,6 @@ struct legend_adamw {
     int device = 0;
     legend_adamw_config cfg{};
     std::vector<legend_adamw_tensor> tensors;
-    std::vector<int32_t> grad_types;
     char* mem = nullptr;                    // everything below, one allocation
     AdamTensor* d_tensors = nullptr;
     const void** d_grads = nullptr;
@@ -86,7 +85,7 @@ int check_matrix(const char* name, const void* p, int64_t stride, int type, int6
     return LEGEND_OK;
 }
 
-int norm_params(legend_ctx* c, const CtxView& v, const legend_layer_norm* n, NormParams* out) {
+int norm_params(const CtxView& v, const legend_layer_norm* n, NormParams* out) {
     if (!n) return fail(LEGEND_E_INVAL, "NULL argument");
     if (n->struct_size != sizeof(legend_layer_norm)) return fail(LEGEND_E_INVAL, "legend_layer_norm.struct_size mismatch");
     if (n->dim < 1 || n->dim > kNormMaxDim) return fail(LEGEND_E_INVAL, "dim must be in [1, %d]", kNormMaxDim);
@@ -125,7 +124,6 @@ int norm_params(legend_ctx* c, const CtxView& v, const legend_layer_norm* n, Nor
     a.weight_type = n->weight_type;
     a.mean = n->mean;
     a.rstd = n->rstd;
-    (void)c;
     *out = a;
     return LEGEND_OK;
 }
@@ -268,7 +266,7 @@ int legend_layer_norm_forward(legend_ctx* c, const legend_layer_norm* n) {
     int rc = ctx_enter(c, &v);
     if (rc) return rc;
     NormParams a;
-    rc = norm_params(c, v, n, &a);
+    rc = norm_params(v, n, &a);
     if (rc) return rc;
     if (!types_go_together(n->x_type, n->y_type)) return fail(LEGEND_E_INVAL, "y_type %d does not go with x_type %d", n->y_type, n->x_type);
     if (n->rows == 0) return LEGEND_OK;
@@ -311,7 +309,7 @@ int legend_layer_norm_backward(legend_ctx* c, const legend_layer_norm* n) {
     int rc = ctx_enter(c, &v);
     if (rc) return rc;
     NormParams a;
-    rc = norm_params(c, v, n, &a);
+    rc = norm_params(v, n, &a);
     if (rc) return rc;
     if (!types_go_together(n->x_type, n->dy_type)) return fail(LEGEND_E_INVAL, "dy_type %d does not go with x_type %d", n->dy_type, n->x_type);
     const bool sums = n->dweight || n->dbias;

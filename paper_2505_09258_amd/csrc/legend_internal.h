@@ -192,7 +192,7 @@ inline int type_size(int t) { return t == LEGEND_TYPE_FLOAT ? 4 : 2; }
 struct CtxView {
     int device = 0;
     hipStream_t stream = nullptr;
-    int dim = 0, num_partitions = 0;
+    int dim = 0;
     int64_t num_nodes = 0, rows_per_partition = 0;
     int32_t relation_rows = 0;
     float* const* part_emb = nullptr;       // device: embedding base per partition or null
@@ -247,6 +247,7 @@ struct AdamState {                          // device; what the next step needs 
     double now_power1, now_power2;
     float scale;                            // of the gradients, and whether the step is skipped: where a kernel
     uint32_t skip;                          // between the two finds them for all workgroups
+    uint32_t ticket;                        // steps of one launch: workgroups that are done
 };
 struct AdamParams {
     const AdamTensor* tensors;

@@ -380,7 +380,6 @@ int ctx_enter(legend_ctx* c, CtxView* v) {
     v->device = c->cfg.device;
     v->stream = c->compute;
     v->dim = c->d;
-    v->num_partitions = c->n;
     v->num_nodes = c->V;
     v->rows_per_partition = c->Rp;
     v->relation_rows = c->nrel_rows;

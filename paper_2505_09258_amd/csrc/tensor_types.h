@@ -17,12 +17,6 @@ template <class T>
 struct Quad {
     typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T))));
 };
-template <class T>
-__device__ inline void load_quad(const T* p, float* out) {
-    const typename Quad<T>::type v = *reinterpret_cast<const typename Quad<T>::type*>(p);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) out[j] = (float)v[j];
-}
 template <bool STREAM = false, class T>
 __device__ inline void store_quad(T* p, const float* in) {
     typename Quad<T>::type v;

@@ -70,7 +70,6 @@ legend_ctx* stub_context(int dim, int64_t nodes, int relations) {
     legend_ctx* c = new legend_ctx;
     c->view.device = 1;
     c->view.dim = dim;
-    c->view.num_partitions = 1;
     c->view.num_nodes = c->view.rows_per_partition = nodes;
     c->view.relation_rows = relations;
     return c;

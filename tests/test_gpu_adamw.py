@@ -264,6 +264,24 @@ def test_states_that_start_at_zero(ctx, block):
     run_steps(ctx, [Tensor(3_000, block=block, zero_state=True)], steps=3)
 
 
+@pytest.mark.parametrize("count", [700, 300_000], ids=str)
+def test_steps_with_and_without_a_norm_in_turn(ctx, count):
+    import torch
+    from paper_2505_09258_amd import binding as L
+    ts = [Tensor(count, block=True), Tensor(40)]
+    opt = L.legend_adamw_create(ctx, [t.describe() for t in ts], seed=4, **HYPER)
+    norm = torch.zeros(1, device="cuda")
+    for step in range(1, 6):
+        before = [t.numbers() for t in ts]
+        torch.cuda.synchronize()
+        L.legend_adamw_step(opt, 0.01, norm=norm.data_ptr() if step in (2, 3, 5) else None)
+        L.legend_sync(ctx)
+        for k, t in enumerate(ts):
+            check_step(t, before[k], step, k, 1.0, 0.01, 4)
+    assert L.legend_adamw_get_steps(opt) == (5, 0)
+    L.legend_adamw_destroy(opt)
+
+
 def test_zero_rate_changes_states_only(ctx):
     t = Tensor(700)
     p = t.param[1].clone()
