@@ -462,9 +462,10 @@ int64_t legend_layer_norm_workspace(int64_t rows, int32_t dim);
  * States: LEGEND_STATE_FLOAT: m, v [count] fp32.  LEGEND_STATE_BLOCK: 8 bits; m and v hold m and sqrt(v) as e4m3 codes (1 sign, 4
  * exponent, 3 mantissa bits, largest 448; 0x7f and 0xff: NaN) in units of an fp32 scale for each block of 256 consecutive
  * elements, scale = max |.| * (1 / 448) over the block's finite values (below 2^-100: 0, and the block's codes too).  The update of p
- * uses the unrounded m and v.  Up to the code every operation is fp32, rounded to nearest, in the order written here.  A value x in units of the scale is rounded stochastically: up from the code below it with the
- * probability of its fraction, so that moments which change by less than a code's step (beta2 = 0.999 changes sqrt(v) by
- * 0.05 % a step, codes are 6 to 12 % apart) still follow on average.  The random word w of element e of tensor k at step t is a
+ * uses the unrounded m and v.  Up to the code every operation is fp32, rounded to nearest, in the order written here.  A
+ * value x in units of the scale is rounded stochastically: up from the code below it with the probability of its
+ * fraction, so that moments which change by less than a code's step (beta2 = 0.999 changes sqrt(v) by 0.05 % a step,
+ * codes are 6 to 12 % apart) still follow on average.  The random word w of element e of tensor k at step t is a
  * counter hash, w = mix(low32(e) ^ low32(e / 2^32) * 0x9E3779B1 ^ low32(fold(fold(seed, t), k))) with fold as in
  * legend_init_partitions and mix(w): w ^= w >> 16, w *= 0x9E3779B1, w ^= w >> 15, w *= 0x85157AF5, w ^= w >> 16 (32 bits); m takes
  * the fraction (w >> 12) / 2^20, sqrt(v) the fraction (w & 0xffff) / 2^16.  A sqrt(v) above zero is at least the smallest code

@@ -282,6 +282,38 @@ def test_steps_with_and_without_a_norm_in_turn(ctx, count):
     L.legend_adamw_destroy(opt)
 
 
+def test_many_steps_at_once_with_and_without_a_norm():
+    """Steps without a norm, 200 workgroups in one launch, against steps whose norm never clips: the same bits, eager and replayed."""
+    import torch
+    from paper_2505_09258_amd import binding as L
+    stream = torch.cuda.Stream()
+    cfg = L.make_config(num_nodes=3, dim=4, batch_size=64, chunk_size=16, num_negs=16, init_std=0.1, seed=1, compute_stream=stream.cuda_stream)
+    c = L.legend_init_partitions(cfg, None, None)
+    try:
+        with torch.cuda.stream(stream):
+            sets = [[Tensor(100_003, 1, 1, True, True), Tensor(101_000, seed=2), Tensor(70, 2, 2)] for _ in range(2)]
+            opts = [L.legend_adamw_create(c, [t.describe() for t in ts], max_norm=m, seed=8, **HYPER) for ts, m in zip(sets, (0.0, 1e30))]
+            stream.synchronize()
+            for o in opts:
+                for _ in range(40):
+                    L.legend_adamw_step(o, 0.001)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                for _ in range(8):
+                    L.legend_adamw_step(opts[0], 0.001)
+            for turn in range(1, 4):
+                graph.replay()
+                for _ in range(8):
+                    L.legend_adamw_step(opts[1], 0.001)
+                for t, u in zip(*sets):
+                    assert all(torch.equal(x, y) for x, y in zip(t.bytes(), u.bytes())), turn
+                assert [L.legend_adamw_get_steps(o) for o in opts] == [(40 + 8 * turn, 0)] * 2
+            for o in opts:
+                L.legend_adamw_destroy(o)
+    finally:
+        L.legend_destroy(c)
+
+
 def test_zero_rate_changes_states_only(ctx):
     t = Tensor(700)
     p = t.param[1].clone()
