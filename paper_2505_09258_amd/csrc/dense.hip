@@ -335,6 +335,7 @@ int legend_layer_norm_backward(legend_ctx* c, const legend_layer_norm* n) {
     }
     bool bad = false;
     if (n->rows > 0) {
+        if (n->table >= 0) written.push_back(bytes_at(n->status, 4));
         if (!n->mean || !n->rstd) return fail(LEGEND_E_INVAL, "mean and rstd of the forward pass must not be NULL");
         Matrix x{}, dy{}, dx{};
         if (n->table < 0) {
@@ -353,8 +354,6 @@ int legend_layer_norm_backward(legend_ctx* c, const legend_layer_norm* n) {
             bad = bad || clash({dx.range}, read);
         }
         bad = bad || clash(written, {x.range, dy.range});
-        if (n->table >= 0) written.push_back(bytes_at(n->status, 4));
-        if (n->dx && n->table >= 0) bad = bad || meets(dx.range, written.back());
         std::vector<Range> shared;
         read_ranges(n, &shared);
         if (n->dx) bad = bad || clash({dx.range}, shared);
