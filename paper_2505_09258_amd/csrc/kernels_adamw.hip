@@ -26,10 +26,9 @@ constexpr uint32_t kLeastNormal = 0x00800000u, kInfinity = 0x7f800000u;     // b
 // Sets of fewer elements are cut into units of 1024, so that more workgroups share them, and their workgroups all fit the card at a
 // time; each adds up the norm's partial sums by itself, which is less than a launch takes.  Larger sets are cut into units of 2048, two
 // blocks in flight a wave (four: 515 against 417 us for 120 M bf16 parameters with 8-bit states, too many registers; units of 2048 for
-// 3 M elements: 28.0 against 24.8), one unit a workgroup (1024 workgroups that take units in turn: 358 against 335 us), and a kernel
-// of one workgroup adds the partial sums up.
+// 3 M elements: 28.0 against 24.8), one unit a workgroup while a launch holds them (1024 workgroups that take units in turn: 358 against
+// 335 us), and a kernel of one workgroup adds the partial sums up.  adam_grid has the numbers of workgroups.
 constexpr int64_t kLargeTotal = 4 << 20;
-constexpr int64_t kGridSmall = 1280;
 constexpr int64_t kGridAlone = 256;         // workgroups that count themselves instead of a launch before them
 // Workgroups of the kernel of the squares.  (120 M elements: 2048 of them read the gradients at 5 TB/s, 1024 at 3.6; 3 M: 24.7 against
 // 25.5 us for the whole step)
@@ -571,7 +570,7 @@ static hipError_t launch_units(hipStream_t st, const AdamParams& a) {
     const int64_t most_parts = K > 1 ? kPartsLarge : kPartsSmall;
     const int parts = (int)(a.units < most_parts ? a.units : most_parts);
     const bool squares = a.with_norm && parts > 0;
-    const int64_t grid = a.units < 1 ? 1 : (K > 1 || a.units < kGridSmall ? a.units : kGridSmall);
+    const int64_t grid = adam_grid(a.units, K > 1);
     if constexpr (K == 1) {
         if (!a.with_norm && grid <= kGridAlone) {
             launch_step<K, STREAM, true>(st, a, grid, 0);

@@ -265,6 +265,13 @@ struct AdamParams {
     int32_t stream;                         // parameters and states are marked as streaming
 };
 int adam_unit_elems(int64_t total);
+// Workgroups of 256 threads of a step's last kernel, which take units in turn: small sets' all fit the card at a time, large sets' have a unit
+// each up to the number that one launch may hold (fewer than 2^32 threads).
+constexpr int64_t kAdamGridSmall = 1280, kAdamGridLarge = (1 << 24) - 1;
+inline int64_t adam_grid(int64_t units, bool large) {
+    const int64_t most = large ? kAdamGridLarge : kAdamGridSmall;
+    return units < 1 ? 1 : (units < most ? units : most);
+}
 void adam_state_at(AdamState* s, int64_t steps, double beta1, double beta2);
 hipError_t launch_adamw(hipStream_t st, const AdamParams& a);
 
