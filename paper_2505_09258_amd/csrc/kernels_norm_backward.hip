@@ -37,12 +37,14 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     RowColumns<XT, S> next_x[R];
     RowColumns<YT, S> next_g[R];
     float next_mean[R], next_rstd[R];
+    bool next_good[R];                           // a table's row that may be read
     RowSource<XT, TABLE, R> source;
     auto load = [&](int64_t r0) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const XT* src = source.row(a, r0, i, lane == 0);
             next_mean[i] = next_rstd[i] = 0.f;
+            next_good[i] = src != nullptr;
             if (src) {
                 next_x[i].load(src, d, lane);
                 next_g[i].load(static_cast<const YT*>(a.dy) + (r0 + i) * a.dy_stride, d, lane);
@@ -69,9 +71,11 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
     }
     for (; r0 < a.rows; r0 += stride) {
         float x[R][NE], g[R][NE], rstd[R];
+        bool good[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             rstd[i] = next_rstd[i];
+            good[i] = !TABLE || next_good[i];
 #pragma unroll
             for (int k = 0; k < NE; ++k) {
                 // (an access behind the row's end holds the row's last columns: what their zero gradients meet is of no account)
@@ -116,7 +120,7 @@ __global__ void __launch_bounds__(S::threads) k_norm_backward(NormParams a) {
             su *= inv_d;
             sx *= inv_d;
 #pragma unroll
-            for (int k = 0; k < NE; ++k) g[i][k] = rstd[i] * fmaf(-x[i][k], sx, g[i][k] - su);
+            for (int k = 0; k < NE; ++k) g[i][k] = good[i] ? rstd[i] * fmaf(-x[i][k], sx, g[i][k] - su) : 0.f;   // (a weight need not be finite)
             store_columns<S>(static_cast<XT*>(a.dx) + (r0 + i) * a.dx_stride, d, lane, g[i]);
         }
     }
