@@ -395,8 +395,9 @@ enum { LEGEND_TYPE_FLOAT = 0, LEGEND_TYPE_BFLOAT = 1, LEGEND_TYPE_HALF = 2 };
  * bits, so that one look at *status covers many calls.  A table's call recorded into a graph reads the partitions where
  * they were when it was recorded: record it again after a swap.
  *
- * A number that is not finite makes its row's y, mean, rstd and dx, and dweight, NaN; numbers beyond 1e18, whose squares leave fp32,
- * make their row's results meaningless, no other row's.
+ * A number that is not finite makes its row's y, mean, rstd and dx, and dweight, NaN; numbers beyond 1e37 / dim, whose sum or rstd
+ * may leave fp32, make their row's results meaningless, no other row's.  Squares below fp32's normal numbers (2^-126) lose digits, which
+ * matters where eps is as small.
  *
  * One struct serves both directions: legend_layer_norm_forward reads the first three groups and writes the last line of the
  * third and the fourth; legend_layer_norm_backward reads mean and rstd as the forward pass wrote them, and the fifth.

@@ -1,11 +1,34 @@
-"""Layer norm at the edges of what it takes.  Tolerances as in test_gpu_layer_norm."""
+"""Layer norm where its numbers run out: rows whose squares leave fp32, and table rows that a call may not read beside a weight
+that is not finite.  Tolerances as in test_gpu_layer_norm: the squares are then summed in units of a power of two, which rounds nothing."""
 
 import numpy as np
 import pytest
 
-from tests.test_gpu_layer_norm import TableCase, check_backward, table_call, tables  # noqa: F401
+from tests.test_gpu_layer_norm import TableCase, Case, backward, check_backward, check_forward, ctx, forward, table_call, tables  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("yt", [0, 1], ids=["f", "b"])
+@pytest.mark.parametrize("dim", [2, 3, 8, 100, 777, 2_000, 4_096, 5_000, 16_384, 20_000, 20_001, 1 << 20], ids=str)
+def test_rows_whose_squares_leave_fp32(ctx, dim, yt):  # noqa: F811
+    """Rows up to the documented 1e37 / dim, between rows of ordinary numbers, which keep their bits."""
+    rng = np.random.default_rng(dim)
+    ordinary = rng.standard_normal((7, dim))
+    x = ordinary.copy()
+    top = 1e37 / dim
+    for r, size in ((1, 0.15 * top), (2, 1e19 if 1e20 < top else 0.01 * top), (4, 3e17)):      # (normal numbers stay within 6 of these)
+        x[r] *= size
+    x[5] = 0.9 * top                                        # but for its first number
+    x[5, 0] = -0.9 * top
+    clean = Case(7, dim, 0, yt, x=ordinary)
+    clean_y, clean_mean, clean_rstd = (t.clone() for t in forward(ctx, clean))
+    case = Case(7, dim, 0, yt, x=x)
+    y, mean, rstd = forward(ctx, case)
+    check_forward(case, y, mean, rstd)
+    for r in (0, 3, 6):
+        assert bool((y[r] == clean_y[r]).all()) and mean[r] == clean_mean[r] and rstd[r] == clean_rstd[r]
+    check_backward(case, backward(ctx, case, mean, rstd), case.x64, case.dy64, mean, rstd)
 
 
 @pytest.mark.parametrize("value", [float("inf"), float("nan")], ids=["inf", "nan"])
