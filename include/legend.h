@@ -449,21 +449,22 @@ int64_t legend_layer_norm_workspace(int64_t rows, int32_t dim);
 /*
  * AdamW over many tensors at once.  With t = steps made + 1, lr' = lr * *lr_factor * lr_scale, every element does
  *   g = grad * *grad_scale * clip
- *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + ((1 - beta2) g) g
  *   p = p (1 - lr' weight_decay) - lr' / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * (decoupled weight decay), where p is the master copy if there is one (the parameter then receives p rounded) and
  *   norm = *grad_scale * sqrt(sum of grad^2 over all tensors)  (64 bits),
  *   clip = max_norm > 0 and norm > max_norm ? max_norm / (norm + 1e-6) : 1.
  * With max_norm > 0 or a norm output asked for, a step whose norm is not finite changes nothing and counts as skipped.
- * Without both the norm is not computed and such gradients go through the formulas.  The root of a v below 2^-126
- * counts as some number below 2^-62; with 8-bit states, a v beyond fp32 makes its element NaN.
+ * Without both the norm is not computed and such gradients go through the formulas.  With 32-bit states the root of a v
+ * below 2^-126 counts as some number below 2^-62; with 8-bit states a v beyond fp32 makes its element NaN.
  * The number of steps lives on the device, so that a recorded step replays as the next one.  Steps of one optimiser must not overlap in
  * time (a graph replayed on another stream than the context's is ordered by the caller).
  *
  * States: LEGEND_STATE_FLOAT: m, v [count] fp32.  LEGEND_STATE_BLOCK: 8 bits; m and v hold m and sqrt(v) as e4m3 codes (1 sign, 4
  * exponent, 3 mantissa bits, largest 448; 0x7f and 0xff: NaN) in units of an fp32 scale for each block of 256 consecutive
  * elements, scale = max |.| * (1 / 448) over the block's finite values (below 2^-100: 0, and the block's codes too).  The update of p
- * uses the unrounded m and v.  Up to the code every operation is fp32, rounded to nearest, in the order written here.  A
+ * uses the unrounded m and v.  Up to the code every operation is fp32, rounded to nearest, in the order written here
+ * (a number below 2^-100 in units of its scale: to within one step of fp32).  A
  * value x in units of the scale is rounded stochastically: up from the code below it with the probability of its
  * fraction, so that moments which change by less than a code's step (beta2 = 0.999 changes sqrt(v) by 0.05 % a step,
  * codes are 6 to 12 % apart) still follow on average.  The random word w of element e of tensor k at step t is a

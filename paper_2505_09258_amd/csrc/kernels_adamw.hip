@@ -21,7 +21,7 @@ namespace legend {
 constexpr float kTopCode = 448.f;           // largest e4m3 value
 constexpr float kLeastCode = 0.001953125f;  // smallest above zero, 2^-9
 constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100: 1 / scale stays far from infinity
-constexpr uint32_t kLeastNormal = 0x00800000u, kInfinity = 0x7f800000u;     // bits of fp32 numbers
+constexpr uint32_t kInfinity = 0x7f800000u;  // bits
 
 // Sets of fewer elements are cut into units of 1024, so that more workgroups share them, and their workgroups all fit the card at a
 // time; each adds up the norm's partial sums by itself, which is less than a launch takes.  Larger sets are cut into units of 2048, two
@@ -160,12 +160,14 @@ __device__ inline void step_float(const Step& s, float g, float& m, float& v, fl
 
 // 8-bit states: every operation up to the code is rounded to nearest once, as it is written (a code depends on the last bit of
 // what it is made from: a root or a quotient that is a bit off is another code once in a million).
-// Root of v: from the hardware's reciprocal root by one step whose residual is exact.  NaN for infinity.
+// Root of v: from the hardware's reciprocal root by one step whose residual is exact; small numbers are lifted, since the residual of one
+// below 2^-102 is not.  That this rounds to nearest was compared for all mantissas of both parities of the exponent.  NaN for infinity.
 __device__ inline float rounded_root(float v) {
-    const float c = __uint_as_float(max(__float_as_uint(v), kLeastNormal));
+    const bool small = v < 0x1p-100f;
+    const float c = v * (small ? 0x1p64f : 1.f);
     const float y = __builtin_amdgcn_rsqf(c);
     const float q = c * y;
-    const float root = fmaf(fmaf(-q, q, c), 0.5f * y, q);
+    const float root = fmaf(fmaf(-q, q, c), 0.5f * y, q) * (small ? 0x1p-32f : 1.f);
     return v > 0.f ? root : v;
 }
 // a / b from y = 1 / b rounded to nearest
