@@ -24,8 +24,13 @@ constexpr float kSmallUnit = 0x1p-96f;            // sums of 2^20 squares of any
 // 1 / sqrt(variance + eps) from the variance of a row that was multiplied by `unit`, a power of two.
 __device__ inline float row_rstd(float var, float eps, float unit) { return 1.f / sqrtf(var + eps * unit * unit) * unit; }
 
+// Waves of a SIMD at most.  Of rows of 2049 to 4096 columns four workgroups a compute unit, so that the grid's eight are two whole rounds: five, which
+// the registers would allow, make the second one a short one (16384 x 4096 bf16 54 against 52.5 us).
+template <class S>
+constexpr int waves_at_most() { return S::NE == 16 && S::T == 256 ? 4 : 8; }
+
 template <class XT, class YT, class S, bool TABLE>
-__global__ void __launch_bounds__(S::threads) k_norm_forward(NormParams a) {
+__global__ void __launch_bounds__(S::threads) __attribute__((amdgpu_waves_per_eu(1, waves_at_most<S>()))) k_norm_forward(NormParams a) {
     constexpr int NE = S::NE, T = S::T, R = S::R;
     __shared__ float box[2][32];
     int turn = 0;
@@ -195,8 +200,9 @@ hipError_t launch_norm_forward(hipStream_t st, const NormParams& a) {
         } else {
             for_shape<1, 256>(a.dim, [&](auto s) {
                 typedef decltype(s) S;
-                // at most the 2048 threads that a compute unit holds, so that weight and bias are loaded once a workgroup (one row a
-                // workgroup: 63 against 51 us for 16384 x 4096 bf16)
+                // at most 2048 threads a compute unit, what it holds of the kernels with up to 64 registers and twice what it holds of those with
+                // up to 128, so that weight and bias are loaded once for several rows (one row a workgroup: 63 against 51 us for 16384 x
+                // 4096 bf16)
                 const int64_t need = (a.rows + S::groups * S::R - 1) / (S::groups * S::R), most = 256 * 2048 / S::threads;
                 const unsigned grid = (unsigned)(need < most ? need : most);
                 if (!a.status) k_norm_forward<XT, YT, S, false><<<grid, S::threads, 0, st>>>(a);
