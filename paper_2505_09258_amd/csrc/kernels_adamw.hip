@@ -162,27 +162,34 @@ __device__ inline void step_float(const Step& s, float g, float& m, float& v, fl
 // what it is made from: a root or a quotient that is a bit off is another code once in a million).
 // Root of v: from the hardware's reciprocal root by one step whose residual is exact; small numbers are lifted, since the residual of one
 // below 2^-102 is not.  That this rounds to nearest was compared for all mantissas of both parities of the exponent.  NaN for infinity.
-__device__ inline float rounded_root(float v) {
-    const bool small = v < 0x1p-100f;
-    const float c = v * (small ? 0x1p64f : 1.f);
-    const float y = __builtin_amdgcn_rsqf(c);
-    const float q = c * y;
-    const float root = fmaf(fmaf(-q, q, c), 0.5f * y, q) * (small ? 0x1p-32f : 1.f);
-    return v > 0.f ? root : v;
+constexpr float kSmallMoment = 0x1p-100f;
+__device__ inline float root_step(float v) {
+    const float y = __builtin_amdgcn_rsqf(v);
+    const float q = v * y;
+    return fmaf(fmaf(-q, q, v), 0.5f * y, q);
+}
+__device__ inline float lifted_root(float v) { return v > 0.f ? root_step(v * 0x1p64f) * 0x1p-32f : v; }
+__device__ inline float rounded_root(float v) { return v < kSmallMoment ? lifted_root(v) : root_step(v); }
+// of four; lifting them all costs 1 % of a step of 120 M bf16 parameters
+__device__ inline void rounded_roots(const float* v, float* root) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) root[j] = root_step(v[j]);
+    if (fminf(fminf(v[0], v[1]), fminf(v[2], v[3])) < kSmallMoment) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) root[j] = v[j] < kSmallMoment ? lifted_root(v[j]) : root[j];
+    }
 }
 // a / b from y = 1 / b rounded to nearest
 __device__ inline float rounded_quotient(float a, float b, float y) {
     const float q = a * y;
     return fmaf(fmaf(-q, b, a), y, q);
 }
-__device__ inline void step_block(const Step& s, float g, float& m, float& v, float& root, float& p) {
+__device__ inline void moments_block(const Step& s, float g, float& m, float& v) {
     g *= s.scale;
     const float m0 = s.b1 * m, m1 = s.c1 * g;
     m = m0 + m1;
     const float v0 = s.b2 * v, v1 = (s.c2 * g) * g;
     v = v0 + v1;
-    root = rounded_root(v);
-    p = step_parameter(s, m, root, p);
 }
 
 // Largest finite magnitudes of a wave's first moments and second moments, and whether some are not finite.
@@ -306,8 +313,13 @@ struct Blocks {
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (BLOCK) step_block(s, ge[j], me[j], ve[j], root[j], pe[j]);
+                if (BLOCK) moments_block(s, ge[j], me[j], ve[j]);
                 else step_float(s, ge[j], me[j], ve[j], pe[j]);
+            }
+            if (BLOCK) {
+                rounded_roots(ve, root);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) pe[j] = step_parameter(s, me[j], root[j], pe[j]);
             }
             if (t.master) store_quad<STREAM>(t.master + i, pe);
             put_quad<STREAM>(t.param, i, t.param_type, pe);
@@ -365,8 +377,13 @@ __device__ inline void part_block(const AdamTensor& t, const void* grad, const S
         }
         float p = t.master ? t.master[i] : load_as(t.param, i, t.param_type);
         const float g = load_as(grad, i, t.grad_type);
-        if (block) step_block(s, g, m[j], v[j], root[j], p);
-        else step_float(s, g, m[j], v[j], p);
+        if (block) {
+            moments_block(s, g, m[j], v[j]);
+            root[j] = rounded_root(v[j]);
+            p = step_parameter(s, m[j], root[j], p);
+        } else {
+            step_float(s, g, m[j], v[j], p);
+        }
         if (t.master) t.master[i] = p;
         store_as(t.param, i, t.param_type, p);
         if (!block) {
