@@ -375,13 +375,15 @@ int64_t legend_rank_edges_static_max_triples(int32_t dim);
  * in device memory of the caller.  These calls
  *   - take DEVICE pointers owned by the caller, on the context's GPU, aligned to their element type;
  *   - enqueue on the context's compute stream and return without waiting.  The caller orders its own streams with that one
- *     (or hands its stream over as legend_config.compute_stream);
+ *     (or hands its stream over as legend_config.compute_stream).  Exception: the first layer norm of table rows after a swap
+ *     re-sends the partition table (one small copy), and waits for the compute stream and with it for the swap's copy;
  *   - allocate nothing, except for legend_adamw_create, and may be recorded into a HIP graph, except where said;
  *   - leave the calling thread's current device as it was;
  *   - give the same bits for the same inputs, whatever runs beside them.
  * A context's rules hold (one thread at a time; LEGEND_E_HIP is final).  Per-kernel profiling does not cover them.
  */
-/* Element types of the caller's device tensors: fp32, bfloat16, fp16.  Arithmetic is fp32, rounded to nearest at the end. */
+/* Element types of the caller's device tensors: fp32, bfloat16, fp16.  Arithmetic is fp32, rounded to nearest at the end; AdamW divides
+ * by the hardware's reciprocal, and with 32-bit states takes its root, each within 1.6 half steps of fp32. */
 enum { LEGEND_TYPE_FLOAT = 0, LEGEND_TYPE_BFLOAT = 1, LEGEND_TYPE_HALF = 2 };
 
 /*
@@ -401,8 +403,12 @@ enum { LEGEND_TYPE_FLOAT = 0, LEGEND_TYPE_BFLOAT = 1, LEGEND_TYPE_HALF = 2 };
  *
  * One struct serves both directions: legend_layer_norm_forward reads the first three groups and writes the last line of the
  * third and the fourth; legend_layer_norm_backward reads mean and rstd as the forward pass wrote them, and the fifth.
+ * dweight and dbias are fp32 sums of up to 72 + rows / 256 terms in turn (rows / 512 where dim <= 4096, rows / 4096 where dim <= 1024),
+ * joined in 64 bits.
+ *
  * Memory: outputs must not overlap anything else the call uses, except that y may be x itself, and dx may be x or dy itself
- * (same address, stride and element size).
+ * (same address, stride and element size).  A matrix counts from its first element to its last, the columns between its rows included:
+ * two halves of the same wide rows are refused.
  */
 typedef struct legend_layer_norm {
     uint32_t struct_size;      /* sizeof(legend_layer_norm) of the caller                          */
@@ -448,7 +454,7 @@ int64_t legend_layer_norm_workspace(int64_t rows, int32_t dim);
 
 /*
  * AdamW over many tensors at once.  With t = steps made + 1, lr' = lr * *lr_factor * lr_scale, every element does
- *   g = grad * *grad_scale * clip
+ *   g = grad * (clip * *grad_scale)          the factor is one fp32 number and loses digits below 2^-126
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + ((1 - beta2) g) g
  *   p = p (1 - lr' weight_decay) - lr' / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * (decoupled weight decay), where p is the master copy if there is one (the parameter then receives p rounded) and
@@ -509,14 +515,14 @@ typedef struct legend_adamw_tensor {
  */
 int legend_adamw_create(legend_ctx* ctx, const legend_adamw_config* cfg, const legend_adamw_tensor* tensors, int64_t n,
                         legend_adamw** out);
-/* Waits for the optimiser's work and frees it.  It may come after legend_destroy of its context (every other call is then
+/* Waits for the optimiser's work and frees it; a graph with its steps must not be replayed any more.  It may come after legend_destroy of its context (every other call is then
  * refused with LEGEND_E_STATE).  NULL is accepted. */
 int legend_adamw_destroy(legend_adamw* opt);
 /* One step.  lr >= 0; lr_factor and grad_scale (>= 0): one fp32 each on the device, read when the step runs, or NULL for 1;
  * norm: one fp32 on the device, or NULL.  None of them may lie in the tensors, states or gradients, nor norm be one of the others. */
 int legend_adamw_step(legend_adamw* opt, double lr, const float* lr_factor, const float* grad_scale, float* norm);
-/* Other gradient buffers for the same tensors, in their order (types as at creation).  Waits for the compute stream; not
- * while it is recording. */
+/* Other gradient buffers for the same tensors, in their order (types as at creation), for recorded steps as well.  Waits for the
+ * compute stream; not while it is recording. */
 int legend_adamw_set_gradients(legend_adamw* opt, const void* const* grads, int64_t n);
 /* Steps made and steps skipped; both wait for the compute stream and are refused while it is recording.  Setting clears the
  * count of skipped steps. */

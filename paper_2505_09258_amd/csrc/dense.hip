@@ -1,5 +1,6 @@
 // Host side of the operators on the caller's own tensors (layer norm, AdamW): argument checks, the optimiser's tables,
-// enqueueing on the context's compute stream.  Nothing here waits or allocates on the way of a forward, backward or step call.
+// enqueueing on the context's compute stream.  Nothing here allocates device memory or waits on the way of a forward, backward or step call,
+// but for the first call on table rows after a swap, which sends the partition table (ctx_tables_current).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -74,7 +75,7 @@ struct Matrix {
     Range range;
 };
 
-// a matrix argument: its range, or an error
+// a matrix argument: its range, the columns between its rows included, or an error
 int check_matrix(const char* name, const void* p, int64_t stride, int type, int64_t rows, int dim, bool repeats, Matrix* m) {
     if (!p) return fail(LEGEND_E_INVAL, "%s must not be NULL", name);
     const int size = type_size(type);

@@ -6,9 +6,9 @@
 //
 // 8-bit states: a wave owns a block of 256 elements, four neighbouring ones a lane; its largest |m| and v set the block's scales.
 //
-// Bound by HBM: 60 M fp32 parameters in 310 us, 5.4 TB/s of what a step cannot do without (first form, one element a thread: 687; with a
+// Bound by HBM: 60 M fp32 parameters in 312 us, 5.4 TB/s of what a step cannot do without (first form, one element a thread: 687; with a
 // counter of finished workgroups at the end, 10 ns a workgroup: 20 us more); 120 M bf16 parameters with master copies and 8-bit states in
-// 350 us, 5.5 TB/s (1476; with divisions and roots as the compiler expands them 490).  The gradients are read twice, the second time from
+// 345 us, 5.6 TB/s (1476; with divisions and roots as the compiler expands them 490).  The gradients are read twice, the second time from
 // the cache where they fit.  Small sets are bound by their launches: 41 000 elements in 8 us, without the norm 5.5.
 #include "legend_internal.h"
 #include "device_utils.h"
