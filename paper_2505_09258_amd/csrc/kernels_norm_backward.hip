@@ -3,9 +3,10 @@
 //   xh = (x - mean) rstd,  u = dy w,  dx = rstd (u - mean(u) - xh mean(u xh)),  dw = sum_rows dy xh,  db = sum_rows dy
 //
 // A row's x and dy stay in the registers of 8 to 512 threads.  A thread keeps the same columns from row to row and adds up its
-// columns' dw and db in fp32 (over rows / 512 rows from 1025 to 4096 columns, rows / 256 above, rows / 4096 and less below); a workgroup writes
-// its sums once, and a second kernel adds those in 64 bits, in a fixed order (no atomics: the same bits every time).  Bound by HBM.  16384 x 4096 bf16: 78 us and 5 for the sums, 5.0 TB/s (first form 1072 us; without
-// the next row's loads ahead 204); 50 000 x 100 table rows, sums only: 11 us and 4 (workgroups of 256 threads: 22 together).
+// columns' dw and db in fp32 (over rows / 512 rows from 1025 to 4096 columns, rows / 256 above, rows / 4096 and less below); a
+// workgroup writes its sums once, and a second kernel adds those in 64 bits, in a fixed order (no atomics: the same bits every
+// time).  Bound by HBM.  16384 x 4096 bf16: 78 us and 5 for the sums, 5.0 TB/s (first form 1072 us; without the next row's loads ahead
+// 204); 50 000 x 100 table rows, sums only: 11 us and 4 (workgroups of 256 threads: 22 together).
 #include "norm_rows.h"
 
 #include <type_traits>
